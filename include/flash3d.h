@@ -79,6 +79,11 @@ extern "C" {
 #define F3D_PROBE_TABLE 1
 #define F3D_PROBE_SEEDED 2
 
+/* Element types of the calls that take more than one (f3d_layer_norm, f3d_clip_grads). */
+#define F3D_BF16 0
+#define F3D_F16 1
+#define F3D_F32 2
+
 #define F3D_MAX_PROBES 6          /* probe offsets of Algorithm 2                                      */
 #define F3D_MAX_SCAN_BUCKETS 8192 /* most hash buckets one scan may own                               */
 #define F3D_MAX_SCOPE_BUCKETS 16  /* most buckets per attention scope                                 */
@@ -284,6 +289,60 @@ int f3d_bucket_swin_attn_bwd(const void *q, const void *k, const void *v, const 
 int f3d_ln_linear(const void *x, const int32_t *row_in, const float *gamma, const float *beta, float eps, const void *w,
                   const float *bias, const void *residual, int64_t n, int32_t c_in, int32_t c_out, void *const *outs,
                   int32_t n_outs, const int32_t *row_out, void *stream);
+
+/*
+ * Layer norm by itself, for training (f3d_ln_linear has it in front of a linear map, without what a backward pass needs):
+ *     y[p] = (x[r] - mean[p]) * rstd[p] * gamma + beta,   r = row_in[p],   rstd = 1 / sqrt(var + eps) (biased variance)
+ *   x           `dtype` [n, channels];  dtype  F3D_BF16 | F3D_F16 | F3D_F32;  channels  1 .. F3D_NORM_MAX_CHANNELS
+ *   row_in      NULL (row p reads x[p]) or [n] int32, e.g. perm: the results come out bucket-major
+ *   gamma, beta binary32 [channels], either may be NULL (ones, zeros)
+ *   eps         >= 0
+ *   y    (out)  `dtype` [n, channels]; may be x where row_in is NULL
+ *   mean, rstd (out)  binary32 [n] of the rows of y, either may be NULL; what f3d_layer_norm_bwd needs
+ * Every pointer is aligned to its elements; where x, y, gamma and beta are 16-byte aligned and a row is a multiple of 16 bytes long
+ * the rows are moved 16 bytes at a time. Arithmetic: binary32, one rounding to dtype. A row's bits do not depend on the others.
+ */
+#define F3D_NORM_MAX_CHANNELS 8192
+int f3d_layer_norm(const void *x, const int32_t *row_in, const float *gamma, const float *beta, float eps, int64_t n,
+                   int32_t channels, int32_t dtype, void *y, float *mean, float *rstd, void *stream);
+
+/*
+ * Backward of f3d_layer_norm: with xh = (x[r] - mean[p]) * rstd[p] and g = dy[p] * gamma,
+ *     dx[r] = rstd[p] * (g - mean(g) - xh * mean(g * xh)) + residual[r],   dgamma = sum_p dy[p] * xh,   dbeta = sum_p dy[p]
+ *   dy          `dtype` [n, channels], row p as in y;  x, row_in, gamma, n, channels, dtype  as in the forward call
+ *   mean, rstd  binary32 [n], the forward call's
+ *   row_in      NULL or a permutation of the rows of x: dx is stored where x was read. Of a row that is named twice one of the two
+ *               results is kept, a row that is not named keeps what dx held
+ *   residual    NULL or `dtype` [n, channels], indexed by the DESTINATION row: the gradient that reaches x past the norm
+ *   dx   (out)  `dtype` [n, channels]; may be residual, and dy or x where row_in is NULL
+ *   dgamma, dbeta (out)  binary32 [channels], either may be NULL; zeros for n = 0
+ *   workspace   >= f3d_layer_norm_bwd_workspace_bytes(n, channels), 256-byte aligned; may be NULL where dgamma and dbeta are
+ * Arithmetic: binary32; the sums over the rows in a fixed order that follows from n, channels and dtype: the same call gives the same bits.
+ */
+int f3d_layer_norm_bwd_workspace_bytes(int64_t n, int32_t channels, size_t *out_bytes);
+
+int f3d_layer_norm_bwd(const void *dy, const void *x, const int32_t *row_in, const float *mean, const float *rstd,
+                       const float *gamma, const void *residual, int64_t n, int32_t channels, int32_t dtype, void *dx,
+                       float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The global norm of a set of gradients and their scaling to a largest norm:
+ *     norm = sqrt(sum over tensors and elements of g^2),   out[t] = g[t] * min(1, max_norm / (norm + 1e-6))
+ *   grads       HOST array of n_tensors DEVICE pointers, aligned to their elements (any elements, in any shape: contiguous)
+ *   outs        NULL: in place. Otherwise a HOST array of DEVICE pointers; an output may be its own gradient, and overlaps no other
+ *               gradient and no other output (refused)
+ *   sizes       HOST array [n_tensors] of element counts, 0 allowed;  dtypes  HOST array [n_tensors] of F3D_BF16 | F3D_F16 | F3D_F32
+ *   n_tensors   0 .. F3D_CLIP_MAX_TENSORS;  max_norm  >= 0, infinity for the norm alone (in place nothing is written then)
+ *   norm (out)  binary32 [1]
+ *   workspace   >= f3d_clip_grads_workspace_bytes(n_tensors), 256-byte aligned. The host arrays may go when the call returns
+ * Squares and sums are held in binary64 and added in a fixed order: no finite gradient overflows, the same call gives the same bits.
+ * A norm that is infinite scales by 0 and one that is NaN by NaN.
+ */
+#define F3D_CLIP_MAX_TENSORS 65536
+int f3d_clip_grads_workspace_bytes(int32_t n_tensors, size_t *out_bytes);
+
+int f3d_clip_grads(const void *const *grads, void *const *outs, const int64_t *sizes, const int32_t *dtypes, int32_t n_tensors,
+                   float max_norm, float *norm, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * In-bucket pooling (Section 4.2 "In-bucket Pooling"; Appendix "In-bucket Pooling"): the bucket-major array is

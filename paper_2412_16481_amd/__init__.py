@@ -24,7 +24,8 @@ ORDERS = {"index": 0, "canonical": 1}
 PROBE_MODES = {"axes": 0, "table": 1, "seeded": 2}
 
 EXPORTS = ("f3d_params_default", "f3d_max_buckets", "f3d_workspace_bytes", "f3d_psh_bucketize", "f3d_psh_bucketize_static",
-           "f3d_bucket_swin_attn", "f3d_bucket_swin_attn_f16", "f3d_attn_block_rows", "f3d_attn_bwd_workspace_bytes", "f3d_bucket_swin_attn_bwd", "f3d_ln_linear", "f3d_pool_max_rows", "f3d_pool_workspace_bytes", "f3d_inbucket_pool",
+           "f3d_bucket_swin_attn", "f3d_bucket_swin_attn_f16", "f3d_attn_block_rows", "f3d_attn_bwd_workspace_bytes", "f3d_bucket_swin_attn_bwd", "f3d_ln_linear",
+           "f3d_layer_norm", "f3d_layer_norm_bwd_workspace_bytes", "f3d_layer_norm_bwd", "f3d_clip_grads_workspace_bytes", "f3d_clip_grads", "f3d_pool_max_rows", "f3d_pool_workspace_bytes", "f3d_inbucket_pool",
            "f3d_unpermute", "f3d_error_string", "f3d_last_hip_error", "f3d_version")
 POOL_OPS = {"sum": 0, "mean": 1, "min": 2, "max": 3}
 
@@ -84,6 +85,16 @@ def lib() -> ctypes.CDLL:
         L.f3d_bucket_swin_attn_bwd.restype = ctypes.c_int
         L.f3d_ln_linear.argtypes = [vp, vp, vp, vp, f32, vp, vp, vp, i64, i32, i32, ctypes.POINTER(vp), i32, vp, vp]
         L.f3d_ln_linear.restype = ctypes.c_int
+        L.f3d_layer_norm.argtypes = [vp, vp, vp, vp, f32, i64, i32, i32, vp, vp, vp, vp]
+        L.f3d_layer_norm.restype = ctypes.c_int
+        L.f3d_layer_norm_bwd_workspace_bytes.argtypes = [i64, i32, ctypes.POINTER(ctypes.c_size_t)]
+        L.f3d_layer_norm_bwd_workspace_bytes.restype = ctypes.c_int
+        L.f3d_layer_norm_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.f3d_layer_norm_bwd.restype = ctypes.c_int
+        L.f3d_clip_grads_workspace_bytes.argtypes = [i32, ctypes.POINTER(ctypes.c_size_t)]
+        L.f3d_clip_grads_workspace_bytes.restype = ctypes.c_int
+        L.f3d_clip_grads.argtypes = [vp, vp, vp, vp, i32, f32, vp, vp, ctypes.c_size_t, vp]
+        L.f3d_clip_grads.restype = ctypes.c_int
         L.f3d_pool_max_rows.argtypes = [i64, i32, i32, i32]
         L.f3d_pool_max_rows.restype = i64
         L.f3d_pool_workspace_bytes.argtypes = [i64, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
@@ -333,6 +344,125 @@ def ln_linear(x, w, bias=None, gamma=None, beta=None, eps: float = 1e-5, row_in=
     if rc != F3D_OK:
         raise Flash3DError(rc, "f3d_ln_linear")
     return outs
+
+
+def _dtypes() -> dict:
+    import torch
+    return {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}   # F3D_BF16, F3D_F16, F3D_F32
+
+
+def _here(*tensors) -> None:
+    """The call's stream is the current device's: tensors of another one would be reached from the wrong queue."""
+    import torch
+    for t in tensors:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, row_in=None, out=None, mean=None, rstd=None):
+    """f3d_layer_norm on torch CUDA tensors. x bfloat16, float16 or float32 [n, channels]; gamma, beta float32 [channels]; row_in
+    int32 [n]. mean, rstd: optional float32 [n] tensors that receive the statistics, for the backward pass. Returns x's type [n, channels]."""
+    import torch
+    if x.dtype not in _dtypes():
+        raise TypeError("x must be bfloat16, float16 or float32")
+    n, c = int(x.shape[0]), int(x.shape[1])
+    _need(x, "x", x.dtype, (n, c))
+    _need(gamma, "gamma", torch.float32, (c,), optional=True)
+    _need(beta, "beta", torch.float32, (c,), optional=True)
+    _need(row_in, "row_in", torch.int32, (n,), optional=True)
+    if out is None:
+        out = torch.empty_like(x)
+    _need(out, "out", x.dtype, (n, c))
+    _need(mean, "mean", torch.float32, (n,), optional=True)
+    _need(rstd, "rstd", torch.float32, (n,), optional=True)
+    _here(x, gamma, beta, row_in, out, mean, rstd)
+    rc = lib().f3d_layer_norm(_ptr(x), _ptr(row_in), _ptr(gamma), _ptr(beta), eps, n, c, _dtypes()[x.dtype], _ptr(out), _ptr(mean),
+                              _ptr(rstd), _stream())
+    if rc != F3D_OK:
+        raise Flash3DError(rc, "f3d_layer_norm")
+    return out
+
+
+def layer_norm_bwd_workspace_bytes(n: int, channels: int) -> int:
+    nb = ctypes.c_size_t(0)
+    rc = lib().f3d_layer_norm_bwd_workspace_bytes(n, channels, ctypes.byref(nb))
+    if rc != F3D_OK:
+        raise Flash3DError(rc, "f3d_layer_norm_bwd_workspace_bytes")
+    return int(nb.value)
+
+
+def layer_norm_bwd(dy, x, mean, rstd, gamma=None, row_in=None, residual=None, weight_grads: bool = True, dx=None, workspace=None):
+    """f3d_layer_norm_bwd. dy, x (and residual) of one type, [n, channels]; mean, rstd float32 [n] from the forward call. Returns (dx,
+    dgamma, dbeta), the last two float32 [channels] or None without weight_grads."""
+    import torch
+    if x.dtype not in _dtypes():
+        raise TypeError("x must be bfloat16, float16 or float32")
+    n, c = int(x.shape[0]), int(x.shape[1])
+    for name, t in (("x", x), ("dy", dy)):
+        _need(t, name, x.dtype, (n, c))
+    _need(mean, "mean", torch.float32, (n,))
+    _need(rstd, "rstd", torch.float32, (n,))
+    _need(gamma, "gamma", torch.float32, (c,), optional=True)
+    _need(row_in, "row_in", torch.int32, (n,), optional=True)
+    _need(residual, "residual", x.dtype, (n, c), optional=True)
+    if dx is None:
+        dx = torch.empty_like(x)
+    _need(dx, "dx", x.dtype, (n, c))
+    dgamma = torch.empty(c, dtype=torch.float32, device=x.device) if weight_grads else None
+    dbeta = torch.empty(c, dtype=torch.float32, device=x.device) if weight_grads else None
+    if workspace is None and weight_grads:
+        workspace = torch.empty(layer_norm_bwd_workspace_bytes(n, c), dtype=torch.uint8, device=x.device)
+    _need(workspace, "workspace", torch.uint8, (None,), optional=True)
+    _here(dy, x, mean, rstd, gamma, row_in, residual, dx, workspace)
+    rc = lib().f3d_layer_norm_bwd(_ptr(dy), _ptr(x), _ptr(row_in), _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(residual), n, c,
+                                  _dtypes()[x.dtype], _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(workspace),
+                                  0 if workspace is None else workspace.numel(), _stream())
+    if rc != F3D_OK:
+        raise Flash3DError(rc, "f3d_layer_norm_bwd")
+    return dx, dgamma, dbeta
+
+
+def clip_grads_workspace_bytes(n_tensors: int) -> int:
+    nb = ctypes.c_size_t(0)
+    rc = lib().f3d_clip_grads_workspace_bytes(n_tensors, ctypes.byref(nb))
+    if rc != F3D_OK:
+        raise Flash3DError(rc, "f3d_clip_grads_workspace_bytes")
+    return int(nb.value)
+
+
+def clip_grads(grads, max_norm: float, outs=None, norm=None, workspace=None):
+    """f3d_clip_grads on a list of contiguous torch CUDA tensors (bfloat16, float16 or float32, mixed as they come): scales them, in
+    place or into `outs`, to a global norm of at most max_norm. Returns the norm before, float32 [1]."""
+    import torch
+    types = _dtypes()
+    n = len(grads)
+    if outs is not None and len(outs) != n:
+        raise ValueError("outs must have as many tensors as grads")
+    device = torch.device("cuda", torch.cuda.current_device())
+    ins, sizes, codes = (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)(), (ctypes.c_int32 * n)()
+    to = None if outs is None else (ctypes.c_void_p * n)()
+    for i, g in enumerate(grads):
+        if g.dtype not in types:
+            raise TypeError(f"grads[{i}] must be bfloat16, float16 or float32")
+        if g.device != device or not g.is_contiguous():
+            raise ValueError(f"grads[{i}] must be a contiguous tensor on {device}")
+        ins[i], sizes[i], codes[i] = g.data_ptr(), g.numel(), types[g.dtype]
+        if to is not None:
+            o = outs[i]
+            if o.dtype != g.dtype or o.shape != g.shape or o.device != device or not o.is_contiguous():
+                raise ValueError(f"outs[{i}] must be contiguous, on {device}, of the type and shape of grads[{i}]")
+            to[i] = o.data_ptr()
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=device)
+    _need(norm, "norm", torch.float32, (1,))
+    if workspace is None:
+        workspace = torch.empty(clip_grads_workspace_bytes(n), dtype=torch.uint8, device=device)
+    _need(workspace, "workspace", torch.uint8, (None,))
+    _here(norm, workspace)
+    rc = lib().f3d_clip_grads(ins, to, sizes, codes, n, max_norm, _ptr(norm), _ptr(workspace), workspace.numel(), _stream())
+    if rc != F3D_OK:
+        raise Flash3DError(rc, "f3d_clip_grads")
+    return norm
 
 
 @dataclass

@@ -5,11 +5,16 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <algorithm>
 #include <atomic>
+#include <memory>
+#include <new>
 
 #include "attn.h"
+#include "clip.h"
 #include "flash3d.h"
 #include "linear.h"
+#include "norm.h"
 #include "pool.h"
 #include "order.h"
 #include "psh.h"
@@ -659,6 +664,165 @@ int f3d_ln_linear(const void* x, const int32_t* row_in, const float* gamma, cons
     a.row_out = row_out;
     (void)hipGetLastError();
     const hipError_t e = f3d::linear_launch(a, (hipStream_t)stream);
+    return e == hipSuccess ? F3D_OK : hip_fail(e);
+}
+
+static int check_norm(int64_t n, int32_t channels, int32_t dtype)
+{
+    if (n < 0 || channels < 1 || dtype < F3D_BF16 || dtype > F3D_F32) return F3D_ERR_INVALID_ARG;
+    if (channels > F3D_NORM_MAX_CHANNELS || n >= (int64_t)2147483647 - (1 << 20)) return F3D_ERR_UNSUPPORTED;
+    return F3D_OK;
+}
+
+static uintptr_t elem_mask(int32_t dtype) { return dtype == F3D_F32 ? 3 : 1; }
+
+int f3d_layer_norm(const void* x, const int32_t* row_in, const float* gamma, const float* beta, float eps, int64_t n, int32_t channels,
+                   int32_t dtype, void* y, float* mean, float* rstd, void* stream)
+{
+    const int rc = check_norm(n, channels, dtype);
+    if (rc != F3D_OK) return rc;
+    if (!(eps >= 0.0f) || !isfinite(eps)) return F3D_ERR_INVALID_ARG;
+    if (n == 0) return F3D_OK;
+    if (!x || !y) return F3D_ERR_INVALID_ARG;
+    if (((uintptr_t)x | (uintptr_t)y) & elem_mask(dtype)) return F3D_ERR_BAD_ALIGNMENT;
+    if (((uintptr_t)row_in | (uintptr_t)gamma | (uintptr_t)beta | (uintptr_t)mean | (uintptr_t)rstd) & 3) return F3D_ERR_BAD_ALIGNMENT;
+    f3d::NormArgs a;
+    memset(&a, 0, sizeof(a));
+    a.x = x;
+    a.row_in = row_in;
+    a.gamma = gamma;
+    a.beta = beta;
+    a.eps = eps;
+    a.n = (int)n;
+    a.c = channels;
+    a.type = dtype;
+    a.wide = !(((uintptr_t)x | (uintptr_t)y | (uintptr_t)gamma | (uintptr_t)beta | ((uintptr_t)channels * (elem_mask(dtype) + 1))) & 15);
+    a.y = y;
+    a.mean = mean;
+    a.rstd = rstd;
+    (void)hipGetLastError();
+    const hipError_t e = f3d::norm_launch(a, (hipStream_t)stream);
+    return e == hipSuccess ? F3D_OK : hip_fail(e);
+}
+
+int f3d_layer_norm_bwd_workspace_bytes(int64_t n, int32_t channels, size_t* out_bytes)
+{
+    if (!out_bytes) return F3D_ERR_INVALID_ARG;
+    const int rc = check_norm(n, channels, F3D_F32);
+    if (rc != F3D_OK) return rc;
+    *out_bytes = align_up((size_t)f3d::norm_bwd_max_blocks(n, channels) * 2 * channels * sizeof(float), 256);
+    return F3D_OK;
+}
+
+int f3d_layer_norm_bwd(const void* dy, const void* x, const int32_t* row_in, const float* mean, const float* rstd, const float* gamma,
+                       const void* residual, int64_t n, int32_t channels, int32_t dtype, void* dx, float* dgamma, float* dbeta,
+                       void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = check_norm(n, channels, dtype);
+    if (rc != F3D_OK) return rc;
+    if (n > 0 && (!dy || !x || !mean || !rstd || !dx)) return F3D_ERR_INVALID_ARG;
+    if (((uintptr_t)dy | (uintptr_t)x | (uintptr_t)residual | (uintptr_t)dx) & elem_mask(dtype)) return F3D_ERR_BAD_ALIGNMENT;
+    if (((uintptr_t)row_in | (uintptr_t)gamma | (uintptr_t)mean | (uintptr_t)rstd | (uintptr_t)dgamma | (uintptr_t)dbeta) & 3)
+        return F3D_ERR_BAD_ALIGNMENT;
+    if (dgamma || dbeta) {
+        if (!workspace) return F3D_ERR_INVALID_ARG;
+        if ((uintptr_t)workspace & 255) return F3D_ERR_BAD_ALIGNMENT;
+        size_t need = 0;
+        f3d_layer_norm_bwd_workspace_bytes(n, channels, &need);
+        if (workspace_bytes < need) return F3D_ERR_WORKSPACE_TOO_SMALL;
+    } else if (n == 0) {
+        return F3D_OK;
+    }
+    f3d::NormBwdArgs a;
+    memset(&a, 0, sizeof(a));
+    a.dy = dy;
+    a.x = x;
+    a.row_in = row_in;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.gamma = gamma;
+    a.residual = residual;
+    a.n = (int)n;
+    a.c = channels;
+    a.type = dtype;
+    a.wide = !(((uintptr_t)dy | (uintptr_t)x | (uintptr_t)residual | (uintptr_t)dx | (uintptr_t)gamma |
+                ((uintptr_t)channels * (elem_mask(dtype) + 1))) & 15);
+    a.dx = dx;
+    a.dgamma = dgamma;
+    a.dbeta = dbeta;
+    a.part = (float*)workspace;
+    (void)hipGetLastError();
+    const hipError_t e = f3d::norm_bwd_launch(a, (hipStream_t)stream);
+    return e == hipSuccess ? F3D_OK : hip_fail(e);
+}
+
+static size_t clip_parts_bytes() { return align_up(f3d::CLIP_MAX_PARTS * sizeof(double), 256); }
+
+int f3d_clip_grads_workspace_bytes(int32_t n_tensors, size_t* out_bytes)
+{
+    if (!out_bytes || n_tensors < 0) return F3D_ERR_INVALID_ARG;
+    if (n_tensors > F3D_CLIP_MAX_TENSORS) return F3D_ERR_UNSUPPORTED;
+    *out_bytes = clip_parts_bytes() + align_up((size_t)n_tensors * sizeof(f3d::ClipTensor), 256);
+    return F3D_OK;
+}
+
+int f3d_clip_grads(const void* const* grads, void* const* outs, const int64_t* sizes, const int32_t* dtypes, int32_t n_tensors,
+                   float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream)
+{
+    size_t need = 0;
+    const int rc = f3d_clip_grads_workspace_bytes(n_tensors, &need);
+    if (rc != F3D_OK) return rc;
+    if (!norm || !workspace || !(max_norm >= 0.0f)) return F3D_ERR_INVALID_ARG;
+    if (n_tensors > 0 && (!grads || !sizes || !dtypes)) return F3D_ERR_INVALID_ARG;
+    if (((uintptr_t)norm & 3) || ((uintptr_t)workspace & 255)) return F3D_ERR_BAD_ALIGNMENT;
+    if (workspace_bytes < need) return F3D_ERR_WORKSPACE_TOO_SMALL;
+    long long chunks = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        if (dtypes[i] < F3D_BF16 || dtypes[i] > F3D_F32 || sizes[i] < 0) return F3D_ERR_INVALID_ARG;
+        if (sizes[i] > ((int64_t)1 << 44)) return F3D_ERR_UNSUPPORTED;
+        if (sizes[i] == 0) continue;
+        const uintptr_t out = (uintptr_t)(outs ? outs[i] : grads[i]);
+        if (!grads[i] || !out) return F3D_ERR_INVALID_ARG;
+        if (((uintptr_t)grads[i] | out) & elem_mask(dtypes[i])) return F3D_ERR_BAD_ALIGNMENT;
+        chunks += f3d::clip_chunks(grads[i], sizes[i], dtypes[i]);
+    }
+    if (chunks > (1ll << 30)) return F3D_ERR_UNSUPPORTED;
+    // an output that shares memory with another tensor would be read or scaled twice, in any order: all ranges by their beginning, every
+    // one against the output and the gradient before it that reach furthest
+    struct Range {
+        uintptr_t from, to;
+        int tensor, out;
+    };
+    const std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[n_tensors > 0 ? 2 * (size_t)n_tensors : 1]);
+    if (!ranges) return F3D_ERR_UNSUPPORTED;
+    size_t n = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        if (sizes[i] == 0) continue;
+        const uintptr_t bytes = (uintptr_t)sizes[i] * (elem_mask(dtypes[i]) + 1), in = (uintptr_t)grads[i];
+        const uintptr_t out = outs ? (uintptr_t)outs[i] : in;
+        ranges[n++] = {out, out + bytes, i, 1};
+        if (out != in) ranges[n++] = {in, in + bytes, i, 0};
+    }
+    std::sort(ranges.get(), ranges.get() + n, [](const Range& a, const Range& b) { return a.from < b.from; });
+    uintptr_t out_end = 0, any_end = 0;
+    for (size_t i = 0; i < n; ++i) {
+        if (ranges[i].from < (ranges[i].out ? any_end : out_end)) return F3D_ERR_INVALID_ARG;
+        any_end = std::max(any_end, ranges[i].to);
+        if (ranges[i].out) out_end = std::max(out_end, ranges[i].to);
+    }
+    f3d::ClipArgs a;
+    memset(&a, 0, sizeof(a));
+    a.in = grads;
+    a.out = outs;
+    a.sizes = sizes;
+    a.types = dtypes;
+    a.tensors = n_tensors;
+    a.max_norm = max_norm;
+    a.norm = norm;
+    a.parts = (double*)workspace;
+    a.table = (f3d::ClipTensor*)((char*)workspace + clip_parts_bytes());
+    (void)hipGetLastError();
+    const hipError_t e = f3d::clip_launch(a, (hipStream_t)stream);
     return e == hipSuccess ? F3D_OK : hip_fail(e);
 }
 

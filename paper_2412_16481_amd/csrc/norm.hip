@@ -1,0 +1,333 @@
+// Layer norm over the channels of every row, forward and backward (Section 4.2, block equations: LN in front of the attention and
+// of the MLP), with the row gather that puts rows into bucket-major order.
+//
+//   forward   y[p] = (x[r] - mu_p) rs_p gamma + beta,  r = row_in[p],  rs_p = 1 / sqrt(var_p + eps)
+//   backward  xh = (x[r] - mu_p) rs_p,  g = dy[p] gamma,
+//             dx[r] = rs_p (g - mean(g) - xh mean(g xh)) + residual[r],
+//             dgamma = sum_p dy[p] xh,  dbeta = sum_p dy[p]
+//
+// A team of 8 to 256 threads holds one row in registers, up to 32 elements each, so a row is read once: the forward takes the mean
+// and then the squares about it, both from the registers (sums of x and x^2 side by side would cancel where a row's mean is large).
+// The backward's teams keep their columns from row to row, so the sums of the weights' gradients stay in registers
+// too; a workgroup adds up its teams at its end and leaves 2 c sums in the workspace, which a second launch adds up in a fixed
+// order: the same call gives the same bits.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "elem.h"
+#include "norm.h"
+
+namespace f3d {
+
+namespace {
+
+constexpr int NTH = 256;      // threads of a workgroup
+
+// Sum over the TPR threads of a team, in every one of them. A team of a whole workgroup joins its waves through LDS: `box` is
+// written again only behind the next barrier of the next sum, so two boxes taken in turn need one barrier a sum.
+template <int TPR>
+__device__ __forceinline__ float team_sum(float v, float* box)
+{
+#pragma unroll
+    for (int d = 1; d < (TPR < 64 ? TPR : 64); d *= 2) v += __shfl_xor(v, d, 64);
+    if (TPR <= 64) return v;
+    if ((threadIdx.x & 63) == 0) box[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (box[0] + box[1]) + (box[2] + box[3]);
+}
+
+template <int TPR>
+__device__ __forceinline__ float2 team_sum2(float v, float w, float* box)
+{
+#pragma unroll
+    for (int d = 1; d < (TPR < 64 ? TPR : 64); d *= 2) {
+        v += __shfl_xor(v, d, 64);
+        w += __shfl_xor(w, d, 64);
+    }
+    if (TPR <= 64) return make_float2(v, w);
+    if ((threadIdx.x & 63) == 0) {
+        box[threadIdx.x >> 6] = v;
+        box[4 + (threadIdx.x >> 6)] = w;
+    }
+    __syncthreads();
+    return make_float2((box[0] + box[1]) + (box[2] + box[3]), (box[4] + box[5]) + (box[6] + box[7]));
+}
+
+// A thread's part of a row: pieces t, t + TPR, .. of W elements. WIDE: 16-byte pieces. Pieces past the row's end count as zeros.
+template <int TYPE, bool WIDE, int TPR, int V>
+struct Part {
+    using E = Elems<TYPE>;
+    using one = typename E::one;
+    static constexpr int W = WIDE ? E::W : 1;
+    static constexpr int N = V * W;                   // elements of a thread
+
+    static __device__ __forceinline__ void load(const one* row, int t, int pieces, float (&x)[N])
+    {
+        if constexpr (WIDE) {
+            uint4 u[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) u[v] = t + v * TPR < pieces ? reinterpret_cast<const uint4*>(row)[t + v * TPR] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int v = 0; v < V; ++v) E::unpack(u[v], *reinterpret_cast<float(*)[W]>(x + v * W));
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = t + v * TPR < pieces ? E::to_f32(row[t + v * TPR]) : 0.f;
+        }
+    }
+    static __device__ __forceinline__ void store(one* row, int t, int pieces, const float (&x)[N])
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (t + v * TPR >= pieces) continue;
+            if constexpr (WIDE) reinterpret_cast<uint4*>(row)[t + v * TPR] = E::pack(*reinterpret_cast<const float(*)[W]>(x + v * W));
+            else row[t + v * TPR] = E::from_f32(x[v]);
+        }
+    }
+    // the row's weights, `none` where there are none
+    static __device__ __forceinline__ void weights(const float* w, float none, int t, int pieces, float (&x)[N])
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int at = (t + v * TPR) * W;
+#pragma unroll
+            for (int e = 0; e < W; ++e) x[v * W + e] = none;
+            if (!w || t + v * TPR >= pieces) continue;
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int e = 0; e < W; e += 4) {
+                    const float4 f = *reinterpret_cast<const float4*>(w + at + e);
+                    x[v * W + e] = f.x;
+                    x[v * W + e + 1] = f.y;
+                    x[v * W + e + 2] = f.z;
+                    x[v * W + e + 3] = f.w;
+                }
+            } else {
+                x[v] = w[at];
+            }
+        }
+    }
+};
+
+template <int TYPE, bool WIDE, int TPR, int V>
+__global__ __launch_bounds__(NTH) void k_norm(NormArgs a)
+{
+    using P = Part<TYPE, WIDE, TPR, V>;
+    using one = typename P::one;
+    constexpr int TEAMS = NTH / TPR;
+    __shared__ float box[2][8];
+    const int t = threadIdx.x % TPR;
+    const long long p = (long long)blockIdx.x * TEAMS + threadIdx.x / TPR;
+    const bool has = p < a.n;                         // a team of 64 threads or fewer may have no row; a workgroup's always has one
+    const int pieces = has ? a.c / P::W : 0;
+    const size_t r = has ? (size_t)(a.row_in ? a.row_in[p] : p) : 0;
+    float x[P::N];
+    P::load(static_cast<const one*>(a.x) + r * a.c, t, pieces, x);
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < P::N; ++i) s += x[i];
+    const float mu = team_sum<TPR>(s, box[0]) / a.c;
+    float q = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        if (t + v * TPR >= pieces) continue;          // the zeros past the end are no elements
+#pragma unroll
+        for (int e = 0; e < P::W; ++e) q += (x[v * P::W + e] - mu) * (x[v * P::W + e] - mu);
+    }
+    const float rs = 1.0f / sqrtf(team_sum<TPR>(q, box[1]) / a.c + a.eps);
+    float g[P::N], b[P::N];
+    P::weights(a.gamma, 1.f, t, pieces, g);
+    P::weights(a.beta, 0.f, t, pieces, b);
+#pragma unroll
+    for (int i = 0; i < P::N; ++i) x[i] = (x[i] - mu) * rs * g[i] + b[i];
+    P::store(static_cast<one*>(a.y) + (size_t)p * a.c, t, pieces, x);
+    if (has && t == 0) {
+        if (a.mean) a.mean[p] = mu;
+        if (a.rstd) a.rstd[p] = rs;
+    }
+}
+
+// WEIGHTS: the sums of the weights' gradients are wanted
+template <int TYPE, bool WIDE, int TPR, int V, bool WEIGHTS>
+__global__ __launch_bounds__(NTH) void k_norm_bwd(NormBwdArgs a)
+{
+    using P = Part<TYPE, WIDE, TPR, V>;
+    using one = typename P::one;
+    constexpr int TEAMS = NTH / TPR;
+    __shared__ float box[2][8];
+    const int t = threadIdx.x % TPR;
+    const int pieces = a.c / P::W;
+    const float inv = 1.0f / a.c;
+    float g[P::N], dg[P::N], db[P::N];
+    P::weights(a.gamma, 1.f, t, pieces, g);
+#pragma unroll
+    for (int i = 0; i < P::N; ++i) dg[i] = db[i] = 0.f;
+    int turn = 0;
+    for (long long p = (long long)blockIdx.x * TEAMS + threadIdx.x / TPR; p < a.n; p += (long long)gridDim.x * TEAMS, turn ^= 1) {
+        const size_t r = (size_t)(a.row_in ? a.row_in[p] : p);
+        float x[P::N], dy[P::N];
+        P::load(static_cast<const one*>(a.dy) + (size_t)p * a.c, t, pieces, dy);
+        P::load(static_cast<const one*>(a.x) + r * a.c, t, pieces, x);
+        const float mu = a.mean[p], rs = a.rstd[p];
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < P::N; ++i) {
+            x[i] = (x[i] - mu) * rs;                  // past the end dy and with it every term is zero
+            if (WEIGHTS) {
+                dg[i] += dy[i] * x[i];
+                db[i] += dy[i];
+            }
+            dy[i] *= g[i];
+            s1 += dy[i];
+            s2 += dy[i] * x[i];
+        }
+        const float2 s = team_sum2<TPR>(s1, s2, box[turn]);
+        const float m1 = s.x * inv, m2 = s.y * inv;
+#pragma unroll
+        for (int i = 0; i < P::N; ++i) dy[i] = rs * (dy[i] - m1 - x[i] * m2);
+        if (a.residual) {
+            P::load(static_cast<const one*>(a.residual) + r * a.c, t, pieces, x);
+#pragma unroll
+            for (int i = 0; i < P::N; ++i) dy[i] += x[i];
+        }
+        P::store(static_cast<one*>(a.dx) + r * a.c, t, pieces, dy);
+    }
+    if (!WEIGHTS) return;
+    // one element of every thread at a time: the teams of a workgroup meet in LDS
+    __shared__ float meet[2][NTH];
+    float* const part = a.part + (size_t)blockIdx.x * 2 * a.c;
+#pragma unroll
+    for (int i = 0; i < P::N; ++i) {
+        if (TEAMS > 1) {
+            __syncthreads();
+            meet[0][threadIdx.x] = dg[i];
+            meet[1][threadIdx.x] = db[i];
+            __syncthreads();
+        }
+        if (threadIdx.x < TPR) {
+            float u = dg[i], w = db[i];
+#pragma unroll
+            for (int k = 1; k < TEAMS; ++k) {
+                u += meet[0][k * TPR + t];
+                w += meet[1][k * TPR + t];
+            }
+            const int piece = t + i / P::W * TPR;
+            if (piece < pieces) {
+                part[piece * P::W + i % P::W] = u;
+                part[a.c + piece * P::W + i % P::W] = w;
+            }
+        }
+    }
+}
+
+// The sums of `blocks` workgroups: 32 columns by 32 groups of workgroups at a time
+__global__ __launch_bounds__(1024) void k_norm_bwd_join(const float* part, int blocks, int c, float* dgamma, float* dbeta)
+{
+    __shared__ float meet[32][33];
+    const int col = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
+    float s = 0.f;
+    if (col < 2 * c) {
+#pragma unroll 8
+        for (int b = k; b < blocks; b += 32) s += part[(size_t)b * 2 * c + col];
+    }
+    meet[k][threadIdx.x & 31] = s;
+    __syncthreads();
+    s = meet[threadIdx.x & 31][k];                    // a wave's half has the 32 sums of one column
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) s += __shfl_xor(s, d, 64);
+    const int of = blockIdx.x * 32 + k;
+    if ((threadIdx.x & 31) == 0 && of < 2 * c) {
+        float* const to = of < c ? dgamma : dbeta;
+        if (to) to[of < c ? of : of - c] = s;
+    }
+}
+
+struct Forward {
+    const NormArgs& a;
+    hipStream_t stream;
+    template <int TYPE, bool WIDE, int TPR, int V>
+    hipError_t go() const
+    {
+        constexpr int TEAMS = NTH / TPR;
+        k_norm<TYPE, WIDE, TPR, V><<<(unsigned)(((long long)a.n + TEAMS - 1) / TEAMS), NTH, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+};
+
+struct Backward {
+    const NormBwdArgs& a;
+    hipStream_t stream;
+    template <int TYPE, bool WIDE, int TPR, int V>
+    hipError_t go() const
+    {
+        constexpr int TEAMS = NTH / TPR;
+        const long long steps = ((long long)a.n + TEAMS - 1) / TEAMS;
+        if (!a.dgamma && !a.dbeta) {
+            k_norm_bwd<TYPE, WIDE, TPR, V, false><<<(unsigned)steps, NTH, 0, stream>>>(a);
+            return hipGetLastError();
+        }
+        // two rows a team at least: a workgroup's sums cost it the write of two rows in binary32
+        const long long most = norm_bwd_max_blocks(a.n, a.c), want = (steps + 1) / 2;
+        const int blocks = (int)(want < most ? want : most);
+        k_norm_bwd<TYPE, WIDE, TPR, V, true><<<(unsigned)blocks, NTH, 0, stream>>>(a);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        k_norm_bwd_join<<<(unsigned)((2 * a.c + 31) / 32), 1024, 0, stream>>>(a.part, blocks, a.c, a.dgamma, a.dbeta);
+        return hipGetLastError();
+    }
+};
+
+// A team is as small as keeps a thread's part of a row in one 16-byte piece, up to a wave, then the parts grow to four pieces, then
+// a workgroup takes the row. Rows that cannot be moved 16 bytes at a time go element by element.
+template <int TYPE, class F>
+hipError_t by_width(const F& f, int c, int wide)
+{
+    if (wide) {
+        const int pieces = c / Elems<TYPE>::W;
+        if (pieces <= 8) return f.template go<TYPE, true, 8, 1>();
+        if (pieces <= 16) return f.template go<TYPE, true, 16, 1>();
+        if (pieces <= 32) return f.template go<TYPE, true, 32, 1>();
+        if (pieces <= 64) return f.template go<TYPE, true, 64, 1>();
+        if (pieces <= 128) return f.template go<TYPE, true, 64, 2>();
+        if (pieces <= 256) return f.template go<TYPE, true, 64, 4>();
+        if (pieces <= 512) return f.template go<TYPE, true, 256, 2>();
+        if (pieces <= 1024) return f.template go<TYPE, true, 256, 4>();
+        if constexpr (TYPE == F3D_F32) return f.template go<TYPE, true, 256, 8>();
+        return hipErrorInvalidValue;
+    }
+    if (c <= 64) return f.template go<TYPE, false, 64, 1>();
+    if (c <= 256) return f.template go<TYPE, false, 64, 4>();
+    if (c <= 1024) return f.template go<TYPE, false, 64, 16>();
+    if (c <= 2048) return f.template go<TYPE, false, 256, 8>();
+    return f.template go<TYPE, false, 256, 32>();
+}
+
+template <class F>
+hipError_t by_type(const F& f, int type, int c, int wide)
+{
+    switch (type) {
+        case F3D_BF16: return by_width<F3D_BF16>(f, c, wide);
+        case F3D_F16: return by_width<F3D_F16>(f, c, wide);
+        default: return by_width<F3D_F32>(f, c, wide);
+    }
+}
+
+}  // namespace
+
+int64_t norm_bwd_max_blocks(int64_t n, int c)
+{
+    const int64_t most = c <= 512 ? 2048 : c <= 2048 ? 1024 : 512, want = (n + 1) / 2;
+    return want < 1 ? 1 : want < most ? want : most;
+}
+
+hipError_t norm_launch(const NormArgs& a, hipStream_t stream) { return by_type(Forward{a, stream}, a.type, a.c, a.wide); }
+
+hipError_t norm_bwd_launch(const NormBwdArgs& a, hipStream_t stream)
+{
+    if (a.n == 0) {   // no rows: the weights' gradients are zero all the same
+        k_norm_bwd_join<<<(unsigned)((2 * a.c + 31) / 32), 1024, 0, stream>>>(a.part, 0, a.c, a.dgamma, a.dbeta);
+        return hipGetLastError();
+    }
+    return by_type(Backward{a, stream}, a.type, a.c, a.wide);
+}
+
+}  // namespace f3d

@@ -1,0 +1,409 @@
+"""Layer norm, its backward and the clipping of gradients on the GPU, through the C ABI, against the definitions in binary64.
+
+Tolerances, with u = 2^-24 (half a step of binary32) and h half a step of the element type relative to the value. A sum over a row or
+over rows is at most 256 additions deep (32 elements of a thread, the 8 steps of a team; up to 40000 / 512 rows of a team, 64 of a
+join and the trees), so its error is at most 256 u times the sum of the magnitudes; x - mean is off by as much of |x| + |mean|.
+"""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2412_16481_amd as f3d
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+
+
+def half(t):
+    return torch.finfo(t).eps / 2
+
+
+def least(t):   # half of the smallest step, near zero
+    return torch.finfo(t).smallest_normal * torch.finfo(t).eps / 2
+
+
+def close(got, want, bound):
+    assert got.shape == want.shape
+    bad = (got.double() - want).abs() - bound
+    assert bool((bad <= 0).all()), f"{int((bad > 0).sum())} of {bad.numel()} outside, by up to {float(bad.max()):.3g}"
+
+
+def make(n, c, t, seed=0, mean=0.5, scale=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed + 1000003 * n + c)
+    r = lambda *s: torch.randn(*s, generator=g, device=DEV)   # noqa: E731
+    return {"x": (r(n, c) * scale + mean * r(c)).to(t), "gamma": 1 + 0.3 * r(c), "beta": 0.3 * r(c), "dy": (0.1 * r(n, c)).to(t),
+            "residual": (0.1 * r(n, c)).to(t), "perm": torch.randperm(n, generator=g, device=DEV).to(torch.int32)}
+
+
+def forward64(x, gamma, beta, eps, row_in):
+    x = x.double() if row_in is None else x.double()[row_in.long()]
+    mean = x.mean(1) if x.shape[1] else x.sum(1)
+    rstd = 1 / torch.sqrt((x - mean[:, None]).square().mean(1) + eps)
+    y = (x - mean[:, None]) * rstd[:, None]
+    if gamma is not None:
+        y = y * gamma.double()
+    return (y if beta is None else y + beta.double()), mean, rstd
+
+
+def check_forward(d, eps=1e-5, gamma=True, beta=True, gather=False):
+    x, t = d["x"], d["x"].dtype
+    n, c = x.shape
+    ga, be, rows = d["gamma"] if gamma else None, d["beta"] if beta else None, d["perm"] if gather else None
+    mean, rstd = torch.full((n,), 7.0, device=DEV), torch.full((n,), 7.0, device=DEV)
+    y = f3d.layer_norm(x, ga, be, eps, rows, mean=mean, rstd=rstd)
+    want, wm, wr = forward64(x, ga, be, eps, rows)
+    xs = x.double() if rows is None else x.double()[rows.long()]
+    most = xs.abs().amax(1) + wm.abs() if c else wm
+    close(mean, wm, 256 * U * xs.abs().mean(1))
+    close(rstd, wr, 256 * U * wr * (1 + wm.abs() * wr))
+    weight = torch.ones(c, device=DEV, dtype=torch.float64) if ga is None else ga.double().abs()
+    close(y, want, half(t) * want.abs() + least(t) + 512 * U * ((most * wr)[:, None] * weight + want.abs()))
+    again = f3d.layer_norm(x, ga, be, eps, rows)
+    assert torch.equal(y, again)
+    return y, mean, rstd
+
+
+def check_backward(d, mean, rstd, gamma=True, gather=False, residual=False, weight_grads=True):
+    x, dy, t = d["x"], d["dy"], d["x"].dtype
+    n, c = x.shape
+    ga, rows, res = d["gamma"] if gamma else None, d["perm"] if gather else None, d["residual"] if residual else None
+    dx = torch.full_like(x, 9.0)
+    _, dgamma, dbeta = f3d.layer_norm_bwd(dy, x, mean, rstd, ga, rows, res, weight_grads, dx=dx)
+    idx = torch.arange(n, device=DEV) if rows is None else rows.long()
+    xs, rs, g0 = x.double()[idx], rstd.double()[:, None], dy.double()
+    xh, X = (xs - mean.double()[:, None]) * rs, (xs.abs() + mean.double().abs()[:, None]) * rs
+    g = g0 if ga is None else g0 * ga.double()
+    row = rs * (g - g.mean(1, keepdim=True) - xh * (g * xh).mean(1, keepdim=True))
+    room = 256 * U * rs * (g.abs() + g.abs().mean(1, keepdim=True) + X * (g.abs() * X).mean(1, keepdim=True))
+    want, bound = torch.zeros_like(xs), torch.zeros_like(xs)
+    want[idx], bound[idx] = row, room
+    if res is not None:
+        want, bound = want + res.double(), bound + 4 * U * res.double().abs()
+    close(dx, want, bound + (half(t) + 2 * U) * want.abs() + least(t))
+    if not weight_grads:
+        assert dgamma is None and dbeta is None
+        return
+    close(dgamma, (g0 * xh).sum(0), 512 * U * (g0.abs() * X).sum(0))
+    close(dbeta, g0.sum(0), 512 * U * g0.abs().sum(0))
+    same = f3d.layer_norm_bwd(dy, x, mean, rstd, ga, rows, res, weight_grads)
+    assert torch.equal(same[0], dx) and torch.equal(same[1], dgamma) and torch.equal(same[2], dbeta)
+
+
+# one width for every form of the kernels, and the widths on both sides of each
+WIDTHS = [1, 7, 16, 64, 65, 72, 128, 136, 255, 256, 264, 512, 520, 1000, 1023, 1024, 1032, 1537, 2048, 2056, 4096, 5001, 8191, 8192]
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("c", WIDTHS)
+def test_layer_norm_widths(c, t):
+    for n, gather, residual in ((1, False, False), (37, True, True), (1000 if c > 600 else 5000, False, True)):
+        d = make(n, c, TYPES[t])
+        _, mean, rstd = check_forward(d, gather=gather)
+        check_backward(d, mean, rstd, gather=gather, residual=residual)
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+def test_layer_norm_without_weights_and_with_every_option(t):
+    for gamma, beta in ((True, False), (False, True), (False, False)):
+        d = make(77, 96, TYPES[t])
+        _, mean, rstd = check_forward(d, gamma=gamma, beta=beta, eps=0.25)
+        check_backward(d, mean, rstd, gamma=gamma, weight_grads=False)
+        check_backward(d, mean, rstd, gamma=gamma, gather=True)
+
+
+@pytest.mark.parametrize("c", [64, 250, 1024, 4096])
+def test_layer_norm_many_rows(c):
+    d = make(40000, c, torch.bfloat16)
+    _, mean, rstd = check_forward(d, gather=True)
+    check_backward(d, mean, rstd, gather=True, residual=True)
+
+
+def test_layer_norm_of_rows_with_a_large_mean_and_of_constant_rows():
+    # sums of squares beside sums would cancel; a constant row has variance zero
+    d = make(300, 256, torch.float32, mean=0.0)
+    d["x"] += 3000.0
+    d["x"][7] = 42.0
+    check_forward(d)
+    x = torch.full((3, 40), 5.0, device=DEV)
+    y = f3d.layer_norm(x, eps=1e-5)
+    assert bool((y == 0).all())
+
+
+def test_layer_norm_rows_do_not_touch_each_other():
+    d = make(50, 200, torch.bfloat16)
+    want = f3d.layer_norm(d["x"], d["gamma"], d["beta"])
+    d["x"][13] = math.nan
+    d["x"][14, 3] = math.inf
+    y = f3d.layer_norm(d["x"], d["gamma"], d["beta"])
+    others = [i for i in range(50) if i not in (13, 14)]
+    assert torch.equal(y[others], want[others]) and bool(y[13:15].isnan().any(1).all())
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+def test_layer_norm_at_addresses_that_are_no_multiple_of_16(t):
+    # tensors that begin inside a larger one, and weights that do: the same values by the other form, and nothing beside them written
+    d = make(41, 128, TYPES[t])
+    y, mean, rstd = check_forward(d)
+    dx, dg, db = f3d.layer_norm_bwd(d["dy"], d["x"], mean, rstd, d["gamma"])
+
+    def moved(x):
+        room = torch.full((x.numel() + 9,), 3.0, dtype=x.dtype, device=DEV)
+        room[1:1 + x.numel()] = x.flatten()
+        return room, room[1:1 + x.numel()].view(x.shape)
+
+    for at in range(4):
+        rooms = [moved(d["x"]), moved(y), moved(d["gamma"]), moved(dx)]
+        x, out, gamma, to = [(r[1] if k == at else v) for k, (r, v) in enumerate(zip(rooms, (d["x"], y.clone(), d["gamma"], dx.clone())))]
+        f3d.layer_norm(x, gamma, d["beta"], out=out)
+        _, dg2, db2 = f3d.layer_norm_bwd(d["dy"], x, mean, rstd, gamma, dx=to)
+        assert float((out.float() - y.float()).abs().max()) <= 4 * half(TYPES[t]) * float(y.float().abs().max())
+        assert float((to.float() - dx.float()).abs().max()) <= 4 * half(TYPES[t]) * float(dx.float().abs().max())
+        assert torch.allclose(dg2, dg, rtol=1e-4, atol=1e-5) and torch.allclose(db2, db, rtol=1e-4, atol=1e-5)
+        for room, x in rooms:
+            assert bool((room[:1] == 3).all()) and bool((room[1 + x.numel():] == 3).all())
+
+
+def test_layer_norm_in_place_and_rows_left_as_they_were():
+    d = make(100, 256, torch.bfloat16)
+    want, mean, rstd = check_forward(d)
+    x = d["x"].clone()
+    assert torch.equal(f3d.layer_norm(x, d["gamma"], d["beta"], out=x), want)
+    want, _, _ = f3d.layer_norm_bwd(d["dy"], d["x"], mean, rstd, d["gamma"], residual=d["residual"])
+    for name in ("residual", "dy", "x"):
+        e = {k: v.clone() for k, v in d.items()}
+        got, _, _ = f3d.layer_norm_bwd(e["dy"], e["x"], mean, rstd, e["gamma"], residual=e["residual"], dx=e[name])
+        assert torch.equal(got, want)
+    # a gather of some rows only, by a call on fewer rows: the others keep what they held
+    rows = d["perm"][:40].contiguous()
+    L = f3d.lib()
+    dx = torch.full_like(d["x"], 5.0)
+    m = torch.empty(40, device=DEV)
+    r = torch.empty(40, device=DEV)
+    y = torch.empty(40, 256, dtype=torch.bfloat16, device=DEV)
+    s = torch.cuda.current_stream().cuda_stream
+    p = lambda t: t.data_ptr()   # noqa: E731
+    assert L.f3d_layer_norm(p(d["x"]), p(rows), p(d["gamma"]), p(d["beta"]), 1e-5, 40, 256, 0, p(y), p(m), p(r), s) == 0
+    assert L.f3d_layer_norm_bwd(p(d["dy"]), p(d["x"]), p(rows), p(m), p(r), p(d["gamma"]), None, 40, 256, 0, p(dx), None, None, None, 0, s) == 0
+    torch.cuda.synchronize()
+    left = torch.ones(100, dtype=torch.bool, device=DEV)
+    left[rows.long()] = False
+    assert bool((dx[left] == 5).all()) and not bool((dx[~left] == 5).all(1).any())
+
+
+def test_layer_norm_of_no_rows():
+    x = torch.empty(0, 64, device=DEV)
+    e = torch.empty(0, device=DEV)
+    assert f3d.layer_norm(x).shape == (0, 64)
+    dx, dg, db = f3d.layer_norm_bwd(x, x, e, e)
+    assert dx.shape == (0, 64) and bool((dg == 0).all()) and bool((db == 0).all())
+
+
+def test_layer_norm_gradients_against_differences():
+    # central differences of the forward pass in binary32 of a scalar function of y; steps of 2^-6 on values of about one: the third
+    # derivative leaves (2^-6)^2 / 6 times a few, the rounding of y 2^-24 * 64 sums / 2^-6
+    n, c = 3, 24
+    d = make(n, c, torch.float32)
+    x, w = d["x"].double().cpu(), d["dy"].double().cpu() * 10
+
+    def value(x, gamma, beta):
+        return float((f3d.layer_norm(x.float().to(DEV), gamma, beta, 0.1).double().cpu() * w).sum())
+
+    mean, rstd = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    f3d.layer_norm(d["x"], d["gamma"], d["beta"], 0.1, mean=mean, rstd=rstd)
+    dx, dg, db = (t.double().cpu() for t in f3d.layer_norm_bwd(w.float().to(DEV), d["x"], mean, rstd, d["gamma"]))
+    step = 2.0 ** -6
+    for i, j in ((0, 0), (1, 5), (2, 23), (2, 11)):
+        up, down = x.clone(), x.clone()
+        up[i, j] += step
+        down[i, j] -= step
+        diff = (value(up, d["gamma"], d["beta"]) - value(down, d["gamma"], d["beta"])) / (2 * step)
+        assert abs(diff - float(dx[i, j])) <= 5e-3
+    for j in (0, 7, 23):
+        for grad, k in ((dg, 0), (db, 1)):
+            up, down = [d["gamma"].clone(), d["beta"].clone()], [d["gamma"].clone(), d["beta"].clone()]
+            up[k][j] += step
+            down[k][j] -= step
+            diff = (value(x, *up) - value(x, *down)) / (2 * step)
+            assert abs(diff - float(grad[j])) <= 1e-3
+
+
+# ----------------------------------------------------------------------------- clipping
+
+
+def clip_case(sizes, types, seed=0, scale=1e-2, gap=0, misalign=False):
+    """Gradients as views of one buffer per type, with `gap` elements between them (and an odd start where misaligned)."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    rooms, views = [], []
+    for k, n in enumerate(sizes):
+        t = TYPES[types[k % len(types)]]
+        first = gap + (k % 5 if misalign else 0)
+        room = torch.full((first + n + gap,), -3.0, dtype=t, device=DEV)
+        room[first:first + n] = (torch.randn(n, generator=g, device=DEV) * scale).to(t)
+        rooms.append(room)
+        views.append(room[first:first + n])
+    return rooms, views
+
+
+def check_clip(grads, max_norm, in_place, out_misaligned=False):
+    before = [x.clone() for x in grads]
+    total = math.sqrt(sum(float(x.double().square().sum()) for x in before))
+    c = min(1.0, max_norm / (total + 1e-6))
+    outs = None
+    if not in_place:
+        outs = [torch.full((x.numel() + 3,), 8.0, dtype=x.dtype, device=DEV)[1 if out_misaligned else 0:][:x.numel()] for x in grads]
+    norm = f3d.clip_grads(grads, max_norm, outs)
+    assert abs(float(norm) - total) <= 4 * U * total
+    for x, old, y in zip(grads, before, grads if in_place else outs):
+        if not in_place:
+            assert torch.equal(x, old)
+        want = old.double() * c
+        close(y, want, (half(x.dtype) + 4 * U) * want.abs() + least(x.dtype))
+    return norm, outs
+
+
+SIZES = {"none": [], "one": [1], "empty": [0, 0, 0], "mixed": [5, 0, 1, 4096, 16383, 16384, 16385, 0, 100001, 8, 3, 2],
+         "128": [77] * 128, "129": [9 + i for i in range(129)], "many": [(37 * i) % 700 for i in range(900)], "long": [3000001, 1, 2500000]}
+
+
+@pytest.mark.parametrize("name", list(SIZES))
+@pytest.mark.parametrize("types", [("bf16",), ("f32",), ("f16", "f32", "bf16")])
+def test_clip_grads_sizes_and_types(name, types):
+    for in_place in (False, True):
+        for max_norm in (0.1, 1e6):
+            rooms, grads = clip_case(SIZES[name], types, gap=3)
+            check_clip(grads, max_norm, in_place)
+            for room, x in zip(rooms, grads):
+                assert bool((room[:3] == -3).all()) and bool((room[3 + x.numel():] == -3).all())
+
+
+@pytest.mark.parametrize("types", [("bf16",), ("f32",), ("f16", "bf16")])
+def test_clip_grads_at_every_alignment(types):
+    sizes = [1, 7, 8, 9, 15, 16, 17, 31, 1000, 40000, 16384, 32768, 5, 16379, 16383]
+    for in_place, out_misaligned in ((True, False), (False, False), (False, True)):
+        rooms, grads = clip_case(sizes, types, gap=4, misalign=True)
+        check_clip(grads, 0.3, in_place, out_misaligned)
+        for k, (room, x) in enumerate(zip(rooms, grads)):
+            first = 4 + k % 5
+            assert bool((room[:first] == -3).all()) and bool((room[first + x.numel():] == -3).all())
+
+
+def test_clip_grads_same_bits_and_no_change_within_the_norm():
+    _, grads = clip_case(SIZES["many"], ("bf16", "f32"))
+    first, outs = check_clip(grads, 0.5, False)
+    again, outs2 = check_clip(grads, 0.5, False)
+    assert torch.equal(first, again) and all(torch.equal(a, b) for a, b in zip(outs, outs2))
+    before = [x.clone() for x in grads]
+    f3d.clip_grads(grads, math.inf)
+    f3d.clip_grads(grads, float(first) * 2)
+    assert all(torch.equal(a, b) for a, b in zip(grads, before))
+
+
+def test_clip_grads_values_whose_squares_leave_binary32():
+    big = [torch.full((1000,), 3e38, device=DEV), torch.full((10,), 1e30, dtype=torch.bfloat16, device=DEV)]
+    norm = f3d.clip_grads(big, 1.0)
+    assert float(norm) == math.inf     # 9.5e39: past binary32, but the scaling knows it
+    assert abs(float(big[0].double().square().sum()) - 1.0) <= 1e-5
+    small = [torch.full((1000,), 1e-30, device=DEV)]
+    norm = f3d.clip_grads(small, 1.0)
+    assert abs(float(norm) - 1e-30 * math.sqrt(1000)) <= 1e-36 and bool((small[0] == 1e-30).all())
+
+
+def test_clip_grads_infinities_and_nan():
+    for bad, others in ((math.inf, 0.0), (math.nan, math.nan)):
+        grads = [torch.ones(100, device=DEV), torch.ones(70000, dtype=torch.bfloat16, device=DEV)]
+        grads[0][3] = bad
+        norm = float(f3d.clip_grads(grads, 1.0))
+        assert norm == math.inf if bad == math.inf else math.isnan(norm)
+        assert math.isnan(float(grads[0][3]))
+        rest = torch.cat([grads[0][:3], grads[0][4:], grads[1].float()])
+        assert bool((rest == 0).all()) if others == 0.0 else bool(rest.isnan().all())
+
+
+def test_clip_grads_outputs_may_be_some_of_the_gradients():
+    _, grads = clip_case([100, 5000, 33], ("f32", "bf16"))
+    want, outs = check_clip(grads, 0.2, False)
+    to = [grads[0], torch.empty_like(grads[1]), grads[2]]
+    norm = f3d.clip_grads(grads, 0.2, to)
+    assert torch.equal(norm, want) and all(torch.equal(a, b) for a, b in zip(to, outs))
+
+
+# ----------------------------------------------------------------------------- streams and graphs
+
+
+def test_norm_and_clip_on_another_stream_and_replayed_from_graphs():
+    # two graphs that share one workspace, replayed in turn with eager calls in between
+    d, e = make(3000, 256, torch.bfloat16), make(500, 256, torch.bfloat16, seed=4)
+    ws = torch.empty(max(f3d.layer_norm_bwd_workspace_bytes(3000, 256), f3d.clip_grads_workspace_bytes(3)), dtype=torch.uint8, device=DEV)
+
+    def step(d, to):
+        f3d.layer_norm(d["x"], d["gamma"], d["beta"], out=to["y"], mean=to["mean"], rstd=to["rstd"])
+        to["dx"], to["dgamma"], to["dbeta"] = f3d.layer_norm_bwd(d["dy"], d["x"], to["mean"], to["rstd"], d["gamma"], dx=to["dx"], workspace=ws)
+        to["norm"] = f3d.clip_grads([to["dx"], to["dgamma"], to["dbeta"]], 0.01, workspace=ws)
+
+    def room(d):
+        n = d["x"].shape[0]
+        return {"y": torch.empty_like(d["x"]), "dx": torch.empty_like(d["x"]), "mean": torch.empty(n, device=DEV), "rstd": torch.empty(n, device=DEV)}
+
+    want = []
+    for c in (d, e):
+        to = room(c)
+        step(c, to)
+        want.append({k: v.clone() for k, v in to.items()})
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    to = room(d)
+    with torch.cuda.stream(side):
+        step(d, to)
+    side.synchronize()
+    assert all(torch.equal(to[k], v) for k, v in want[0].items())
+    graphs, rooms = [], [room(d), room(e)]
+    for c, to in zip((d, e), rooms):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(c, to)
+        graphs.append(graph)
+    for _ in range(3):
+        for graph, to, w in zip(graphs, rooms, want):
+            to["dx"].fill_(1.0)
+            to["norm"].fill_(-1.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(to[k], v) for k, v in w.items())
+            step(e, room(e))
+            torch.cuda.synchronize()
+
+
+def test_norm_and_clip_refusals_by_the_binding():
+    x = torch.zeros(4, 8, device=DEV)
+    with pytest.raises(TypeError):
+        f3d.layer_norm(x.double())
+    with pytest.raises(ValueError):
+        f3d.layer_norm(torch.zeros(8, 4, device=DEV).t())
+    with pytest.raises(ValueError):
+        f3d.layer_norm(x.cpu())
+    with pytest.raises(ValueError):
+        f3d.layer_norm(x, gamma=torch.zeros(7, device=DEV))
+    with pytest.raises(TypeError):
+        f3d.layer_norm_bwd(x.bfloat16(), x, torch.zeros(4, device=DEV), torch.zeros(4, device=DEV))
+    with pytest.raises(f3d.Flash3DError) as err:
+        f3d.layer_norm(torch.zeros(1, 8193, device=DEV))
+    assert err.value.code == f3d.ERR_UNSUPPORTED
+    with pytest.raises(f3d.Flash3DError) as err:
+        f3d.clip_grads([x, x], 1.0)
+    assert err.value.code == f3d.ERR_INVALID_ARG
+    with pytest.raises(f3d.Flash3DError):
+        f3d.clip_grads([x, x.clone()], 1.0, [x.clone(), x])
+    with pytest.raises(ValueError):
+        f3d.clip_grads([x.t()], 1.0)
+    with pytest.raises(TypeError):
+        f3d.clip_grads([x.long()], 1.0)
+    ws = torch.empty(256, dtype=torch.uint8, device=DEV)
+    with pytest.raises(f3d.Flash3DError) as err:
+        f3d.clip_grads([x], 1.0, workspace=ws)
+    assert err.value.code == f3d.ERR_WORKSPACE_TOO_SMALL
+    assert ctypes.sizeof(ctypes.c_void_p) == 8
