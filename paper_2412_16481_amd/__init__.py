@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from dataclasses import dataclass
 from typing import Optional
 
@@ -422,6 +423,10 @@ def layer_norm_bwd(dy, x, mean, rstd, gamma=None, row_in=None, residual=None, we
     return dx, dgamma, dbeta
 
 
+def _at(a) -> Optional[int]:
+    return None if a is None else a.buffer_info()[0]
+
+
 def clip_grads_workspace_bytes(n_tensors: int) -> int:
     nb = ctypes.c_size_t(0)
     rc = lib().f3d_clip_grads_workspace_bytes(n_tensors, ctypes.byref(nb))
@@ -434,24 +439,23 @@ def clip_grads(grads, max_norm: float, outs=None, norm=None, workspace=None):
     """f3d_clip_grads on a list of contiguous torch CUDA tensors (bfloat16, float16 or float32, mixed as they come): scales them, in
     place or into `outs`, to a global norm of at most max_norm. Returns the norm before, float32 [1]."""
     import torch
-    types = _dtypes()
-    n = len(grads)
-    if outs is not None and len(outs) != n:
-        raise ValueError("outs must have as many tensors as grads")
-    device = torch.device("cuda", torch.cuda.current_device())
-    ins, sizes, codes = (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)(), (ctypes.c_int32 * n)()
-    to = None if outs is None else (ctypes.c_void_p * n)()
-    for i, g in enumerate(grads):
-        if g.dtype not in types:
-            raise TypeError(f"grads[{i}] must be bfloat16, float16 or float32")
-        if g.device != device or not g.is_contiguous():
-            raise ValueError(f"grads[{i}] must be a contiguous tensor on {device}")
-        ins[i], sizes[i], codes[i] = g.data_ptr(), g.numel(), types[g.dtype]
-        if to is not None:
-            o = outs[i]
-            if o.dtype != g.dtype or o.shape != g.shape or o.device != device or not o.is_contiguous():
-                raise ValueError(f"outs[{i}] must be contiguous, on {device}, of the type and shape of grads[{i}]")
-            to[i] = o.data_ptr()
+    T, types, n, here = torch.Tensor, _dtypes(), len(grads), torch.cuda.current_device()
+    device = torch.device("cuda", here)
+    # hundreds of tensors: what is asked of each is asked of all at once, and only a refusal looks for the one it is about
+    sizes = array("q", map(T.numel, grads))
+    kinds = [g.dtype for g in grads]
+    try:
+        codes = array("i", map(types.__getitem__, kinds))
+    except KeyError:
+        raise TypeError("grads must be bfloat16, float16 or float32") from None
+    if outs is not None and (len(outs) != n or array("q", map(T.numel, outs)) != sizes or [o.dtype for o in outs] != kinds):
+        raise ValueError("outs must be as many tensors as grads, each of the type and size of its gradient")
+    for name, ts in (("grads", grads), ("outs", outs)):
+        if ts is not None and not (all(map(T.is_contiguous, ts)) and set(map(T.get_device, ts)) <= {here}):
+            i = next(i for i, t in enumerate(ts) if t.get_device() != here or not t.is_contiguous())
+            raise ValueError(f"{name}[{i}] must be a contiguous tensor on {device}")
+    ins = array("Q", map(T.data_ptr, grads))
+    to = None if outs is None else array("Q", map(T.data_ptr, outs))
     if norm is None:
         norm = torch.empty(1, dtype=torch.float32, device=device)
     _need(norm, "norm", torch.float32, (1,))
@@ -459,7 +463,7 @@ def clip_grads(grads, max_norm: float, outs=None, norm=None, workspace=None):
         workspace = torch.empty(clip_grads_workspace_bytes(n), dtype=torch.uint8, device=device)
     _need(workspace, "workspace", torch.uint8, (None,))
     _here(norm, workspace)
-    rc = lib().f3d_clip_grads(ins, to, sizes, codes, n, max_norm, _ptr(norm), _ptr(workspace), workspace.numel(), _stream())
+    rc = lib().f3d_clip_grads(_at(ins), _at(to), _at(sizes), _at(codes), n, max_norm, _ptr(norm), _ptr(workspace), workspace.numel(), _stream())
     if rc != F3D_OK:
         raise Flash3DError(rc, "f3d_clip_grads")
     return norm

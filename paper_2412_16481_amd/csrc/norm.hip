@@ -22,6 +22,7 @@ namespace f3d {
 namespace {
 
 constexpr int NTH = 256;      // threads of a workgroup
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 // Sum over the TPR threads of a team, in every one of them. A team of a whole workgroup joins its waves through LDS: `box` is
 // written again only behind the next barrier of the next sum, so two boxes taken in turn need one barrier a sum.
@@ -74,13 +75,21 @@ struct Part {
             for (int v = 0; v < V; ++v) x[v] = t + v * TPR < pieces ? E::to_f32(row[t + v * TPR]) : 0.f;
         }
     }
+    template <bool STREAMED = false>
     static __device__ __forceinline__ void store(one* row, int t, int pieces, const float (&x)[N])
     {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (t + v * TPR >= pieces) continue;
-            if constexpr (WIDE) reinterpret_cast<uint4*>(row)[t + v * TPR] = E::pack(*reinterpret_cast<const float(*)[W]>(x + v * W));
-            else row[t + v * TPR] = E::from_f32(x[v]);
+            if constexpr (WIDE) {
+                const uint4 u = E::pack(*reinterpret_cast<const float(*)[W]>(x + v * W));
+                const u32x4 y = {u.x, u.y, u.z, u.w};
+                u32x4* const to = reinterpret_cast<u32x4*>(row) + t + v * TPR;
+                if (STREAMED) __builtin_nontemporal_store(y, to);
+                else *to = y;
+            } else {
+                row[t + v * TPR] = E::from_f32(x[v]);
+            }
         }
     }
     // the row's weights, `none` where there are none
@@ -108,52 +117,71 @@ struct Part {
     }
 };
 
-template <int TYPE, bool WIDE, int TPR, int V>
+// R rows a team, all requested before the first is looked at. STREAMED: results past the caches
+template <int TYPE, bool WIDE, int TPR, int V, int R, bool STREAMED>
 __global__ __launch_bounds__(NTH) void k_norm(NormArgs a)
 {
     using P = Part<TYPE, WIDE, TPR, V>;
     using one = typename P::one;
     constexpr int TEAMS = NTH / TPR;
-    __shared__ float box[2][8];
+    __shared__ float box[2 * R][8];
     const int t = threadIdx.x % TPR;
-    const long long p = (long long)blockIdx.x * TEAMS + threadIdx.x / TPR;
-    const bool has = p < a.n;                         // a team of 64 threads or fewer may have no row; a workgroup's always has one
-    const int pieces = has ? a.c / P::W : 0;
-    const size_t r = has ? (size_t)(a.row_in ? a.row_in[p] : p) : 0;
-    float x[P::N];
-    P::load(static_cast<const one*>(a.x) + r * a.c, t, pieces, x);
-    float s = 0.f;
+    const long long first = (long long)blockIdx.x * (TEAMS * R) + threadIdx.x / TPR;
+    const int pieces = a.c / P::W;
+    size_t r[R];
 #pragma unroll
-    for (int i = 0; i < P::N; ++i) s += x[i];
-    const float mu = team_sum<TPR>(s, box[0]) / a.c;
-    float q = 0.f;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        if (t + v * TPR >= pieces) continue;          // the zeros past the end are no elements
-#pragma unroll
-        for (int e = 0; e < P::W; ++e) q += (x[v * P::W + e] - mu) * (x[v * P::W + e] - mu);
+    for (int k = 0; k < R; ++k) {
+        const long long p = min(first + k * TEAMS, (long long)a.n - 1);   // past the end: the last row again, which is not stored
+        r[k] = (size_t)(a.row_in ? a.row_in[p] : p);
     }
-    const float rs = 1.0f / sqrtf(team_sum<TPR>(q, box[1]) / a.c + a.eps);
+    float x[R][P::N];
+#pragma unroll
+    for (int k = 0; k < R; ++k) P::load(static_cast<const one*>(a.x) + r[k] * a.c, t, pieces, x[k]);
     float g[P::N], b[P::N];
     P::weights(a.gamma, 1.f, t, pieces, g);
     P::weights(a.beta, 0.f, t, pieces, b);
+    const float inv = 1.0f / a.c;
+    float mu[R], rs[R];
 #pragma unroll
-    for (int i = 0; i < P::N; ++i) x[i] = (x[i] - mu) * rs * g[i] + b[i];
-    P::store(static_cast<one*>(a.y) + (size_t)p * a.c, t, pieces, x);
-    if (has && t == 0) {
-        if (a.mean) a.mean[p] = mu;
-        if (a.rstd) a.rstd[p] = rs;
+    for (int k = 0; k < R; ++k) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < P::N; ++i) s += x[k][i];
+        mu[k] = team_sum<TPR>(s, box[k]) * inv;
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        float q = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (t + v * TPR >= pieces) continue;      // the zeros past the end are no elements
+#pragma unroll
+            for (int e = 0; e < P::W; ++e) q += (x[k][v * P::W + e] - mu[k]) * (x[k][v * P::W + e] - mu[k]);
+        }
+        rs[k] = 1.0f / sqrtf(team_sum<TPR>(q, box[R + k]) * inv + a.eps);
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const long long p = first + k * TEAMS;
+        if (p >= a.n) break;
+#pragma unroll
+        for (int i = 0; i < P::N; ++i) x[k][i] = (x[k][i] - mu[k]) * rs[k] * g[i] + b[i];
+        P::template store<STREAMED>(static_cast<one*>(a.y) + (size_t)p * a.c, t, pieces, x[k]);
+        if (t == 0) {
+            if (a.mean) a.mean[p] = mu[k];
+            if (a.rstd) a.rstd[p] = rs[k];
+        }
     }
 }
 
 // WEIGHTS: the sums of the weights' gradients are wanted
-template <int TYPE, bool WIDE, int TPR, int V, bool WEIGHTS>
+template <int TYPE, bool WIDE, int TPR, int V, int R, bool WEIGHTS, bool STREAMED>
 __global__ __launch_bounds__(NTH) void k_norm_bwd(NormBwdArgs a)
 {
     using P = Part<TYPE, WIDE, TPR, V>;
     using one = typename P::one;
     constexpr int TEAMS = NTH / TPR;
-    __shared__ float box[2][8];
+    __shared__ float box[2 * R][8];
     const int t = threadIdx.x % TPR;
     const int pieces = a.c / P::W;
     const float inv = 1.0f / a.c;
@@ -162,34 +190,51 @@ __global__ __launch_bounds__(NTH) void k_norm_bwd(NormBwdArgs a)
 #pragma unroll
     for (int i = 0; i < P::N; ++i) dg[i] = db[i] = 0.f;
     int turn = 0;
-    for (long long p = (long long)blockIdx.x * TEAMS + threadIdx.x / TPR; p < a.n; p += (long long)gridDim.x * TEAMS, turn ^= 1) {
-        const size_t r = (size_t)(a.row_in ? a.row_in[p] : p);
-        float x[P::N], dy[P::N];
-        P::load(static_cast<const one*>(a.dy) + (size_t)p * a.c, t, pieces, dy);
-        P::load(static_cast<const one*>(a.x) + r * a.c, t, pieces, x);
-        const float mu = a.mean[p], rs = a.rstd[p];
-        float s1 = 0.f, s2 = 0.f;
+    for (long long first = (long long)blockIdx.x * (TEAMS * R) + threadIdx.x / TPR; first < a.n; first += (long long)gridDim.x * (TEAMS * R), turn ^= R) {
+        size_t r[R];
+        float x[R][P::N], dy[R][P::N], mu[R], rs[R];
 #pragma unroll
-        for (int i = 0; i < P::N; ++i) {
-            x[i] = (x[i] - mu) * rs;                  // past the end dy and with it every term is zero
-            if (WEIGHTS) {
-                dg[i] += dy[i] * x[i];
-                db[i] += dy[i];
+        for (int k = 0; k < R; ++k) {
+            const bool has = first + k * TEAMS < a.n;  // past the end: zeros
+            const long long p = has ? first + k * TEAMS : 0;
+            r[k] = (size_t)(has && a.row_in ? a.row_in[p] : p);
+            mu[k] = has ? a.mean[p] : 0.f;
+            rs[k] = has ? a.rstd[p] : 0.f;
+            P::load(static_cast<const one*>(a.dy) + (size_t)p * a.c, t, has ? pieces : 0, dy[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) P::load(static_cast<const one*>(a.x) + r[k] * a.c, t, first + k * TEAMS < a.n ? pieces : 0, x[k]);
+        float m1[R], m2[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < P::N; ++i) {
+                x[k][i] = (x[k][i] - mu[k]) * rs[k];  // past the row's end dy and with it every term is zero
+                if (WEIGHTS) {
+                    dg[i] += dy[k][i] * x[k][i];
+                    db[i] += dy[k][i];
+                }
+                dy[k][i] *= g[i];
+                s1 += dy[k][i];
+                s2 += dy[k][i] * x[k][i];
             }
-            dy[i] *= g[i];
-            s1 += dy[i];
-            s2 += dy[i] * x[i];
+            const float2 s = team_sum2<TPR>(s1, s2, box[turn + k]);
+            m1[k] = s.x * inv;
+            m2[k] = s.y * inv;
         }
-        const float2 s = team_sum2<TPR>(s1, s2, box[turn]);
-        const float m1 = s.x * inv, m2 = s.y * inv;
 #pragma unroll
-        for (int i = 0; i < P::N; ++i) dy[i] = rs * (dy[i] - m1 - x[i] * m2);
-        if (a.residual) {
-            P::load(static_cast<const one*>(a.residual) + r * a.c, t, pieces, x);
+        for (int k = 0; k < R; ++k) {
+            if (first + k * TEAMS >= a.n) break;
 #pragma unroll
-            for (int i = 0; i < P::N; ++i) dy[i] += x[i];
+            for (int i = 0; i < P::N; ++i) dy[k][i] = rs[k] * (dy[k][i] - m1[k] - x[k][i] * m2[k]);
+            if (a.residual) {
+                P::load(static_cast<const one*>(a.residual) + r[k] * a.c, t, pieces, x[k]);
+#pragma unroll
+                for (int i = 0; i < P::N; ++i) dy[k][i] += x[k][i];
+            }
+            P::template store<STREAMED>(static_cast<one*>(a.dx) + r[k] * a.c, t, pieces, dy[k]);
         }
-        P::store(static_cast<one*>(a.dx) + r * a.c, t, pieces, dy);
     }
     if (!WEIGHTS) return;
     // one element of every thread at a time: the teams of a workgroup meet in LDS
@@ -219,27 +264,29 @@ __global__ __launch_bounds__(NTH) void k_norm_bwd(NormBwdArgs a)
     }
 }
 
-// The sums of `blocks` workgroups: 32 columns by 32 groups of workgroups at a time
+// The sums of `blocks` workgroups: 16 columns by 64 groups of workgroups at a time
 __global__ __launch_bounds__(1024) void k_norm_bwd_join(const float* part, int blocks, int c, float* dgamma, float* dbeta)
 {
-    __shared__ float meet[32][33];
-    const int col = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
+    __shared__ float meet[64][17];
+    const int col = blockIdx.x * 16 + (threadIdx.x & 15), k = threadIdx.x >> 4;
     float s = 0.f;
     if (col < 2 * c) {
-#pragma unroll 8
-        for (int b = k; b < blocks; b += 32) s += part[(size_t)b * 2 * c + col];
+#pragma unroll 16
+        for (int b = k; b < blocks; b += 64) s += part[(size_t)b * 2 * c + col];
     }
-    meet[k][threadIdx.x & 31] = s;
+    meet[k][threadIdx.x & 15] = s;
     __syncthreads();
-    s = meet[threadIdx.x & 31][k];                    // a wave's half has the 32 sums of one column
+    s = meet[threadIdx.x & 63][threadIdx.x >> 6];     // a wave has the 64 sums of one column
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) s += __shfl_xor(s, d, 64);
-    const int of = blockIdx.x * 32 + k;
-    if ((threadIdx.x & 31) == 0 && of < 2 * c) {
+    for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d, 64);
+    const int of = blockIdx.x * 16 + (threadIdx.x >> 6);
+    if ((threadIdx.x & 63) == 0 && of < 2 * c) {
         float* const to = of < c ? dgamma : dbeta;
         if (to) to[of < c ? of : of - c] = s;
     }
 }
+
+constexpr size_t STREAMED_BYTES = (size_t)4 << 20;
 
 struct Forward {
     const NormArgs& a;
@@ -247,8 +294,12 @@ struct Forward {
     template <int TYPE, bool WIDE, int TPR, int V>
     hipError_t go() const
     {
-        constexpr int TEAMS = NTH / TPR;
-        k_norm<TYPE, WIDE, TPR, V><<<(unsigned)(((long long)a.n + TEAMS - 1) / TEAMS), NTH, 0, stream>>>(a);
+        constexpr int TEAMS = NTH / TPR, R = TPR == 256 || !WIDE ? 1 : 4 / V;
+        const long long steps = ((long long)a.n + TEAMS - 1) / TEAMS;
+        if (WIDE && (size_t)a.n * a.c * sizeof(typename Elems<TYPE>::one) >= STREAMED_BYTES)
+            k_norm<TYPE, WIDE, TPR, V, R, WIDE><<<(unsigned)((steps + R - 1) / R), NTH, 0, stream>>>(a);
+        else
+            k_norm<TYPE, WIDE, TPR, V, 1, false><<<(unsigned)steps, NTH, 0, stream>>>(a);
         return hipGetLastError();
     }
 };
@@ -256,23 +307,33 @@ struct Forward {
 struct Backward {
     const NormBwdArgs& a;
     hipStream_t stream;
-    template <int TYPE, bool WIDE, int TPR, int V>
-    hipError_t go() const
+    template <int TYPE, bool WIDE, int TPR, int V, int R, bool STREAMED>
+    hipError_t with() const
     {
-        constexpr int TEAMS = NTH / TPR;
+        constexpr int TEAMS = NTH / TPR * R;
         const long long steps = ((long long)a.n + TEAMS - 1) / TEAMS;
         if (!a.dgamma && !a.dbeta) {
-            k_norm_bwd<TYPE, WIDE, TPR, V, false><<<(unsigned)steps, NTH, 0, stream>>>(a);
+            k_norm_bwd<TYPE, WIDE, TPR, V, R, false, STREAMED><<<(unsigned)steps, NTH, 0, stream>>>(a);
             return hipGetLastError();
         }
         // two rows a team at least: a workgroup's sums cost it the write of two rows in binary32
-        const long long most = norm_bwd_max_blocks(a.n, a.c), want = (steps + 1) / 2;
+        const long long most = norm_bwd_max_blocks(a.n, a.c), want = (steps * R + 1) / 2;
         const int blocks = (int)(want < most ? want : most);
-        k_norm_bwd<TYPE, WIDE, TPR, V, true><<<(unsigned)blocks, NTH, 0, stream>>>(a);
-        hipError_t e = hipGetLastError();
+        k_norm_bwd<TYPE, WIDE, TPR, V, R, true, STREAMED><<<(unsigned)blocks, NTH, 0, stream>>>(a);
+        const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        k_norm_bwd_join<<<(unsigned)((2 * a.c + 31) / 32), 1024, 0, stream>>>(a.part, blocks, a.c, a.dgamma, a.dbeta);
+        k_norm_bwd_join<<<(unsigned)((2 * a.c + 15) / 16), 1024, 0, stream>>>(a.part, blocks, a.c, a.dgamma, a.dbeta);
         return hipGetLastError();
+    }
+    template <int TYPE, bool WIDE, int TPR, int V>
+    hipError_t go() const
+    {
+        constexpr int R = TPR == 256 || !WIDE || V > 2 ? 1 : 2;
+        const bool large = (size_t)a.n * a.c * sizeof(typename Elems<TYPE>::one) >= STREAMED_BYTES;
+        if constexpr (WIDE) {
+            if (large) return with<TYPE, WIDE, TPR, V, R, true>();
+        }
+        return with<TYPE, WIDE, TPR, V, 1, false>();
     }
 };
 
@@ -315,7 +376,7 @@ hipError_t by_type(const F& f, int type, int c, int wide)
 
 int64_t norm_bwd_max_blocks(int64_t n, int c)
 {
-    const int64_t most = c <= 512 ? 2048 : c <= 2048 ? 1024 : 512, want = (n + 1) / 2;
+    const int64_t most = c <= 2048 ? 1024 : 512, want = (n + 1) / 2;
     return want < 1 ? 1 : want < most ? want : most;
 }
 
@@ -324,7 +385,7 @@ hipError_t norm_launch(const NormArgs& a, hipStream_t stream) { return by_type(F
 hipError_t norm_bwd_launch(const NormBwdArgs& a, hipStream_t stream)
 {
     if (a.n == 0) {   // no rows: the weights' gradients are zero all the same
-        k_norm_bwd_join<<<(unsigned)((2 * a.c + 31) / 32), 1024, 0, stream>>>(a.part, 0, a.c, a.dgamma, a.dbeta);
+        k_norm_bwd_join<<<(unsigned)((2 * a.c + 15) / 16), 1024, 0, stream>>>(a.part, 0, a.c, a.dgamma, a.dbeta);
         return hipGetLastError();
     }
     return by_type(Backward{a, stream}, a.type, a.c, a.wide);
