@@ -267,6 +267,66 @@ int f3d_bucket_swin_attn_bwd(const void *q, const void *k, const void *v, const 
                              const int32_t *grad_perm, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Attention to states of another length: the query rows of segment b (the points of a scan, the tokens of a sequence, one row of a
+ * decoder) attend to all key/value rows of segment b (pooled points, image or text states, a cache), as many or few as there are:
+ *     S = softmax_scale * q k^T,  lse = log sum_keys exp S,  out = exp(S - lse) v
+ * for every head; heads h * G .. h * G + G - 1 share key/value head h, G = heads / kv_heads.
+ *
+ *   q           bf16 [n_q, heads*head_dim];  k, v  bf16 [n_kv, kv_heads*head_dim], all 16-byte aligned
+ *   q_offsets   [n_segments+1] int32, non-decreasing: segment b owns query rows q_offsets[b] .. q_offsets[b+1]-1. The batch_offsets of
+ *               scans serve as they are (bucket-major rows keep them). NULL = one segment of all rows
+ *   kv_offsets  the same for the key/value rows, e.g. pooled_offsets of f3d_inbucket_pool
+ *   q_lens, kv_lens  NULL or [n_segments] int32: only the first q_lens[b] / kv_lens[b] rows of a segment take part (a padded batch,
+ *               a cache that is not full). What lies behind them is not read into any result, NaN included
+ *   n_segments  1 .. 65535;  max_q, max_kv  upper bounds, known on the host, on the rows of a segment (0: n_q, n_kv). They choose the
+ *               form of the launch; with a segment that is longer its results are unspecified
+ *   heads, kv_heads  heads a multiple of kv_heads;  head_dim  16, 32, 64 or 128;  softmax_scale  0 = 1/sqrt(head_dim)
+ *   out  (out)  bf16 [n_q, heads*head_dim];  lse (out)  NULL or binary32 [n_q, heads], what f3d_cross_attn_bwd needs
+ *               A row without keys gets zeros, and lse -infinity; so does a row behind its segment's q_lens. Rows before the first
+ *               segment and behind the last keep what they held
+ *   workspace   >= f3d_cross_attn_workspace_bytes(...) of the same sizes, 256-byte aligned; may be NULL where that is 0
+ * Inconsistent offsets or lengths give unspecified results but no access out of bounds. out overlaps no input.
+ * Arithmetic: 16-bit operands, fp32 accumulation and softmax (the running maximum followed within 2^8), the sum of the exponentials
+ * taken in fp32, the probabilities rounded to 16 bits before the product with v; one rounding of the result. Inputs must be finite, and
+ * so must their scaled scores in binary32. The same call gives the same bits; how the keys are split follows from n_q, n_segments,
+ * max_q, max_kv, heads, kv_heads and head_dim.
+ */
+int f3d_cross_attn_workspace_bytes(int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q, int64_t max_kv, int32_t heads,
+                                   int32_t kv_heads, int32_t head_dim, size_t *out_bytes);
+
+int f3d_cross_attn(const void *q, const void *k, const void *v, const int32_t *q_offsets, const int32_t *kv_offsets,
+                   const int32_t *q_lens, const int32_t *kv_lens, int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q,
+                   int64_t max_kv, int32_t heads, int32_t kv_heads, int32_t head_dim, float softmax_scale, void *out, float *lse,
+                   void *workspace, size_t workspace_bytes, void *stream);
+
+/* The same on IEEE binary16 tensors. softmax_scale * log2(e) is limited to 2^90 (every score is finite then). Forward only. */
+int f3d_cross_attn_f16(const void *q, const void *k, const void *v, const int32_t *q_offsets, const int32_t *kv_offsets,
+                       const int32_t *q_lens, const int32_t *kv_lens, int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q,
+                       int64_t max_kv, int32_t heads, int32_t kv_heads, int32_t head_dim, float softmax_scale, void *out, float *lse,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Backward of f3d_cross_attn:
+ *     P = exp(S - lse),  dP = dout v^T,  D = rowsum(dout o out),  dS = P o (dP - D),
+ *     dq = scale dS k,   dk = scale sum over the heads that share it of dS^T q,   dv = the same sum of P^T dout
+ *   q .. softmax_scale   as in the forward call;  out, dout  bf16 [n_q, heads*head_dim];  lse  the forward call's
+ *   dq (out)  bf16 [n_q, heads*head_dim];  dk, dv (out)  bf16 [n_kv, kv_heads*head_dim]. Rows behind a segment's length get zeros, and
+ *             so do rows of no segment and everything of a segment without queries or without keys. The gradients overlap no input and
+ *             not each other
+ *   workspace >= f3d_cross_attn_bwd_workspace_bytes(...) of the same sizes, 256-byte aligned
+ * Arithmetic: bf16 operands, fp32 accumulation; P and dS are rounded to bf16 before the second products. Sums over rows, heads and
+ * parts are added in a fixed order: the same call gives the same bits.
+ */
+int f3d_cross_attn_bwd_workspace_bytes(int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q, int64_t max_kv, int32_t heads,
+                                       int32_t kv_heads, int32_t head_dim, size_t *out_bytes);
+
+int f3d_cross_attn_bwd(const void *q, const void *k, const void *v, const void *out, const void *dout, const float *lse,
+                       const int32_t *q_offsets, const int32_t *kv_offsets, const int32_t *q_lens, const int32_t *kv_lens, int64_t n_q,
+                       int64_t n_kv, int32_t n_segments, int64_t max_q, int64_t max_kv, int32_t heads, int32_t kv_heads,
+                       int32_t head_dim, float softmax_scale, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,
+                       void *stream);
+
+/*
  * The point-wise glue of a transformer block (Section 4.2, block equations F' = MHSA(LN(F)) + F, F~ = MLP(LN(F')) + F';
  * Section 4.1 "Stage Orchestration"): LayerNorm and a linear map over every row in one pass, with the row gather that
  * writes q, k, v in bucket-major order and the row scatter + residual that brings a block's output back.

@@ -26,6 +26,7 @@ PROBE_MODES = {"axes": 0, "table": 1, "seeded": 2}
 
 EXPORTS = ("f3d_params_default", "f3d_max_buckets", "f3d_workspace_bytes", "f3d_psh_bucketize", "f3d_psh_bucketize_static",
            "f3d_bucket_swin_attn", "f3d_bucket_swin_attn_f16", "f3d_attn_block_rows", "f3d_attn_bwd_workspace_bytes", "f3d_bucket_swin_attn_bwd", "f3d_ln_linear",
+           "f3d_cross_attn_workspace_bytes", "f3d_cross_attn", "f3d_cross_attn_f16", "f3d_cross_attn_bwd_workspace_bytes", "f3d_cross_attn_bwd",
            "f3d_layer_norm", "f3d_layer_norm_bwd_workspace_bytes", "f3d_layer_norm_bwd", "f3d_clip_grads_workspace_bytes", "f3d_clip_grads", "f3d_pool_max_rows", "f3d_pool_workspace_bytes", "f3d_inbucket_pool",
            "f3d_unpermute", "f3d_error_string", "f3d_last_hip_error", "f3d_version")
 POOL_OPS = {"sum": 0, "mean": 1, "min": 2, "max": 3}
@@ -86,6 +87,17 @@ def lib() -> ctypes.CDLL:
         L.f3d_bucket_swin_attn_bwd.restype = ctypes.c_int
         L.f3d_ln_linear.argtypes = [vp, vp, vp, vp, f32, vp, vp, vp, i64, i32, i32, ctypes.POINTER(vp), i32, vp, vp]
         L.f3d_ln_linear.restype = ctypes.c_int
+        sizes = [i64, i64, i32, i64, i64, i32, i32, i32]
+        L.f3d_cross_attn_workspace_bytes.argtypes = sizes + [ctypes.POINTER(ctypes.c_size_t)]
+        L.f3d_cross_attn_workspace_bytes.restype = ctypes.c_int
+        L.f3d_cross_attn.argtypes = [vp] * 7 + sizes + [f32, vp, vp, vp, ctypes.c_size_t, vp]
+        L.f3d_cross_attn.restype = ctypes.c_int
+        L.f3d_cross_attn_f16.argtypes = L.f3d_cross_attn.argtypes
+        L.f3d_cross_attn_f16.restype = ctypes.c_int
+        L.f3d_cross_attn_bwd_workspace_bytes.argtypes = sizes + [ctypes.POINTER(ctypes.c_size_t)]
+        L.f3d_cross_attn_bwd_workspace_bytes.restype = ctypes.c_int
+        L.f3d_cross_attn_bwd.argtypes = [vp] * 10 + sizes + [f32, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.f3d_cross_attn_bwd.restype = ctypes.c_int
         L.f3d_layer_norm.argtypes = [vp, vp, vp, vp, f32, i64, i32, i32, vp, vp, vp, vp]
         L.f3d_layer_norm.restype = ctypes.c_int
         L.f3d_layer_norm_bwd_workspace_bytes.argtypes = [i64, i32, ctypes.POINTER(ctypes.c_size_t)]
@@ -318,6 +330,83 @@ def bucket_swin_attn_bwd(q, k, v, out, dout, lse, buckets: Buckets, heads: int, 
                                         _ptr(buckets.perm) if original_order else None, _ptr(workspace), workspace.numel(), _stream())
     if rc != F3D_OK:
         raise Flash3DError(rc, "f3d_bucket_swin_attn_bwd")
+    return dq, dk, dv
+
+
+def cross_attn_workspace_bytes(n_q: int, n_kv: int, n_segments: int, max_q: int, max_kv: int, heads: int, kv_heads: int, head_dim: int,
+                               backward: bool = False) -> int:
+    """f3d_cross_attn_workspace_bytes, or with `backward` f3d_cross_attn_bwd_workspace_bytes."""
+    name = "f3d_cross_attn_bwd_workspace_bytes" if backward else "f3d_cross_attn_workspace_bytes"
+    nb = ctypes.c_size_t(0)
+    rc = getattr(lib(), name)(n_q, n_kv, n_segments, max_q, max_kv, heads, kv_heads, head_dim, ctypes.byref(nb))
+    if rc != F3D_OK:
+        raise Flash3DError(rc, name)
+    return int(nb.value)
+
+
+def _cross_sizes(q, k, v, q_offsets, kv_offsets, heads, head_dim, kv_heads, max_q, max_kv, q_lens, kv_lens):
+    """The checks both cross attention calls share; the sizes as the C calls take them."""
+    import torch
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("q, k, v must be bfloat16 or float16")
+    kv_heads = heads if kv_heads is None else kv_heads
+    n_q, n_kv = int(q.shape[0]), int(k.shape[0])
+    _need(q, "q", q.dtype, (n_q, heads * head_dim))
+    _need(k, "k", q.dtype, (n_kv, kv_heads * head_dim))
+    _need(v, "v", q.dtype, (n_kv, kv_heads * head_dim))
+    segments = {int(t.shape[0]) - less for t, less in ((q_offsets, 1), (kv_offsets, 1), (q_lens, 0), (kv_lens, 0)) if t is not None} or {1}
+    if len(segments) != 1 or ((q_offsets is None or kv_offsets is None) and segments != {1}):
+        raise ValueError("q_offsets, kv_offsets (one more entry than segments), q_lens and kv_lens must be of the same segments")
+    n_segments = segments.pop()
+    for name, t, n in (("q_offsets", q_offsets, n_segments + 1), ("kv_offsets", kv_offsets, n_segments + 1), ("q_lens", q_lens, n_segments),
+                       ("kv_lens", kv_lens, n_segments)):
+        _need(t, name, torch.int32, (n,), optional=True)
+    return n_q, n_kv, n_segments, max_q, max_kv, heads, kv_heads, head_dim
+
+
+def cross_attn(q, k, v, q_offsets, kv_offsets, heads: int, head_dim: int, kv_heads: Optional[int] = None, max_q: int = 0, max_kv: int = 0,
+               q_lens=None, kv_lens=None, softmax_scale: float = 0.0, out=None, lse=None, workspace=None):
+    """f3d_cross_attn (bfloat16 tensors) or f3d_cross_attn_f16 (float16 tensors), by the dtype of q. q: [n_q, heads*head_dim]; k, v:
+    [n_kv, kv_heads*head_dim]; offsets: int32 [segments + 1] or None (one segment); lens: int32 [segments] or None. max_q, max_kv: the
+    longest segment's rows or a bound on them (0: n_q, n_kv). lse: optional float32 [n_q, heads] tensor that receives the rows'
+    log-sum-exp, for the backward pass. Returns [n_q, heads*head_dim] of the same type."""
+    import torch
+    sizes = _cross_sizes(q, k, v, q_offsets, kv_offsets, heads, head_dim, kv_heads, max_q, max_kv, q_lens, kv_lens)
+    if out is None:
+        out = torch.empty_like(q)
+    _need(out, "out", q.dtype, tuple(q.shape))
+    _need(lse, "lse", torch.float32, (sizes[0], heads), optional=True)
+    if workspace is None:
+        need = cross_attn_workspace_bytes(*sizes)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _need(workspace, "workspace", torch.uint8, (None,), optional=True)
+    _here(q, k, v, q_offsets, kv_offsets, q_lens, kv_lens, out, lse, workspace)
+    entry = lib().f3d_cross_attn if q.dtype == torch.bfloat16 else lib().f3d_cross_attn_f16
+    rc = entry(_ptr(q), _ptr(k), _ptr(v), _ptr(q_offsets), _ptr(kv_offsets), _ptr(q_lens), _ptr(kv_lens), *sizes, softmax_scale, _ptr(out),
+               _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
+    if rc != F3D_OK:
+        raise Flash3DError(rc, "f3d_cross_attn")
+    return out
+
+
+def cross_attn_bwd(q, k, v, out, dout, lse, q_offsets, kv_offsets, heads: int, head_dim: int, kv_heads: Optional[int] = None, max_q: int = 0,
+                   max_kv: int = 0, q_lens=None, kv_lens=None, softmax_scale: float = 0.0, workspace=None):
+    """f3d_cross_attn_bwd, bfloat16. out, lse: the forward call's; dout: [n_q, heads*head_dim]. Returns (dq, dk, dv)."""
+    import torch
+    sizes = _cross_sizes(q, k, v, q_offsets, kv_offsets, heads, head_dim, kv_heads, max_q, max_kv, q_lens, kv_lens)
+    for name, t in (("q", q), ("out", out), ("dout", dout)):
+        _need(t, name, torch.bfloat16, tuple(q.shape))
+    _need(lse, "lse", torch.float32, (sizes[0], heads))
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    if workspace is None:
+        workspace = torch.empty(max(cross_attn_workspace_bytes(*sizes, backward=True), 256), dtype=torch.uint8, device=q.device)
+    _need(workspace, "workspace", torch.uint8, (None,))
+    _here(q, k, v, out, dout, lse, q_offsets, kv_offsets, q_lens, kv_lens, workspace)
+    rc = lib().f3d_cross_attn_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(dout), _ptr(lse), _ptr(q_offsets), _ptr(kv_offsets), _ptr(q_lens),
+                                  _ptr(kv_lens), *sizes, softmax_scale, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace), workspace.numel(),
+                                  _stream())
+    if rc != F3D_OK:
+        raise Flash3DError(rc, "f3d_cross_attn_bwd")
     return dq, dk, dv
 
 

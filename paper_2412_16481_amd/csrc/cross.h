@@ -1,0 +1,61 @@
+// Internal interface between the C ABI (flash3d_api.hip) and the cross attention kernels (cross.hip, cross_bwd.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "attn.h"
+
+namespace f3d {
+
+struct CrossArgs {
+    const uint16_t* q;
+    const uint16_t* k;
+    const uint16_t* v;
+    const int32_t* q_offsets;   // [segments + 1]
+    const int32_t* kv_offsets;
+    const int32_t* q_lens;      // null, or [segments]
+    const int32_t* kv_lens;
+    int n_q, n_kv;
+    int segments;
+    int H, K, G;                // heads, key/value heads, heads that share one of these
+    Divide by_g;                // rows of a segment, heads that share keys counted one by one, by G
+    float q_pow2;               // bfloat16: a power of two, at most 1, that goes into the query (exactly), and
+    float s_mul;                // what is left of scale * log2(e), multiplied onto the score
+    uint16_t* out;
+    float* lse;                 // null, or [n_q, H]
+    int f16;
+    int few;                    // the form for few query rows
+    int row_tiles;              // tiles of 32 query rows a wave owns
+    int slots;                  // row blocks over all segments (upper bound, surplus workgroups exit)
+    int parts;                  // parts the keys of a segment are split into
+    int chunk;                  // keys of a part
+    float* part_o;              // [parts][n_q * H][head_dim], sums of a part relative to its largest score
+    float2* part_ml;            // [parts][n_q * H]: that score (log2 units), sum of exponentials
+};
+
+struct CrossBwdArgs {
+    CrossArgs f;                // parts and chunk of the query gradient's kernel
+    const uint16_t* dout;
+    float* dsum;                // [n_q, H]: sum over the head's channels of dout * out
+    uint16_t* dq;
+    uint16_t* dk;
+    uint16_t* dv;
+    float scale;
+    float* part_dq;             // [parts][n_q * H][head_dim], where parts > 1
+    int kv_slots;               // blocks of 128 keys over all segments
+    int row_parts;              // parts the query rows of a segment are split into
+    int row_chunk;              // rows of a part
+    float* part_dkv;            // [2][row_parts][n_kv * K][head_dim], where row_parts > 1
+};
+
+// What a call takes: a rule on sizes the host knows
+struct CrossPlan {
+    int few, row_tiles, slots, parts, chunk;
+    int kv_slots, row_parts, row_chunk;   // backward
+};
+CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_q, long long max_kv, int heads, int kv_heads, int head_dim, bool backward);
+
+hipError_t cross_launch(const CrossArgs& a, int head_dim, hipStream_t stream);
+hipError_t cross_bwd_launch(const CrossBwdArgs& a, int head_dim, hipStream_t stream);
+
+}  // namespace f3d

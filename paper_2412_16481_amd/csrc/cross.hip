@@ -1,0 +1,427 @@
+// Cross attention forward for gfx950 (Section 4.2's attention, with the keys of another set): the query rows of a segment (the points
+// of a scan, the tokens of a sequence) attend to all states of the same segment, of which there are another number.
+//
+//   S = scale q k^T,  P = exp(S - lse),  lse = log sum exp S,  out = P v
+//
+// Heads that share a key/value head are rows below each other: row r of a (segment, key/value head) is query r / G and head r % G of
+// the group, so a state is read once for all of them. A wave owns tiles of 32 such rows; keys and values stream through LDS in
+// stages filled by global -> LDS loads a stage ahead, row-major, swizzled (cross_common.h). Per tile of 32 keys the TRANSPOSED score
+// tile S^T = K Q^T comes from 32x32x16 MFMAs: a lane then owns 16 keys of ONE row, its exponentials are per-lane work, and the
+// probabilities, rounded to 16 bits, are the B operand of O^T += V^T P^T as they lie. The running maximum moves the reference of a row's
+// exponentials only when a score exceeds it by more than 2^8, so O is rarely rescaled; the sum of the exponentials is taken before
+// they are rounded.
+//
+// Two forms. ROWS: every wave has rows of its own and all keys. FEW: a (segment, key/value head) has one tile of rows or less, the four
+// waves take the four key tiles of a stage and meet in LDS at the end; that form reads keys as fast as memory delivers them, which
+// is all a call with single queries does. Where the launch would leave compute units idle the keys are split into parts, whose
+// results (relative to the part's largest score) a second kernel joins in a fixed order.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "cross_common.h"
+
+namespace f3d {
+
+namespace {
+
+constexpr float LN2 = 0.6931471805599453f;
+
+template <int D, bool FEW>
+struct Stage {
+    using T = Tile<D>;
+    static constexpr int ROWS = !FEW && D == 128 ? 64 : 128;   // keys
+    static constexpr int TILES = ROWS / 32;
+    static constexpr int BYTES = ROWS * T::ROWB;               // of K, and of V
+    static constexpr int NBUF = D >= 64 ? 2 : 3;
+    static constexpr int LPW = ROWS * T::NC / 256;             // loads per lane, stage and tensor
+    static constexpr int TOTAL = NBUF * 2 * BYTES;
+};
+
+template <int D, int QT, bool FEW, bool F16, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a)
+{
+    using T = Tile<D>;
+    using S = Stage<D, FEW>;
+    using E = Half<F16>;
+    constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF;
+    constexpr int BM = FEW ? 32 : 128 * QT, SHIFT = FEW ? 5 : QT == 2 ? 8 : 7;   // rows of a workgroup
+    static_assert(!FEW || QT == 1, "one tile of rows");
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[S::TOTAL];
+    const uint32_t sK = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sV = sK + NBUF * S::BYTES;
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    // which (row block, part, key/value head): consecutive ids stay on one XCD, the heads of the same rows beside each other
+    const uint32_t u = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    const uint32_t x = u / (uint32_t)a.K;
+    const int kh = (int)(u - x * a.K), slot = (int)(SPLIT ? x / (uint32_t)a.parts : x), part = SPLIT ? (int)(x - (uint32_t)slot * a.parts) : 0;
+    if (slot >= a.slots) return;
+    const int b = segment_of(a.q_offsets, a.n_q, a.segments, a.G, SHIFT, slot);
+    const Rows qs = rows_of(a.q_offsets, a.q_lens, a.n_q, b), ks_ = rows_of(a.kv_offsets, a.kv_lens, a.n_kv, b);
+    const long long blk = slot - first_slot(a.q_offsets, a.n_q, b, a.G, SHIFT);
+    const long long rows = (long long)qs.span * a.G, live = (long long)qs.len * a.G;
+    if (blk < 0 || blk * BM >= rows) return;
+    const int key0 = SPLIT ? part * a.chunk : 0;
+    const int nkeys = blk * BM >= live ? 0 : SPLIT ? min(max(ks_.len - key0, 0), a.chunk) : ks_.len;   // this workgroup's
+
+    // ---- staging
+    const uint32_t row_bytes = (uint32_t)a.K * T::ROWB;
+    const uint64_t first = (uint64_t)(ks_.from + key0) * row_bytes + (uint64_t)kh * T::ROWB;
+    int srow[LPW];
+    uint32_t scol[LPW];
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+        const int p = (wave * LPW + i) * 64 + lane;
+        srow[i] = p / T::NC;
+        scol[i] = ((p % T::NC) ^ T::swizzle(srow[i])) << 4;
+    }
+    auto dma_stage = [&](int st) __attribute__((always_inline)) {
+        const uint32_t to = (st % NBUF) * S::BYTES;
+#pragma unroll
+        for (int i = 0; i < LPW; ++i) {
+            const int key = min(st * S::ROWS + srow[i], nkeys - 1);   // past the end: the last key again, masked
+            const uint64_t at = first + (uint64_t)(uint32_t)key * row_bytes + scol[i];
+            lds_dma16(reinterpret_cast<const char*>(a.k) + at, sK + to + (wave * LPW + i) * 1024);
+            lds_dma16(reinterpret_cast<const char*>(a.v) + at, sV + to + (wave * LPW + i) * 1024);
+        }
+    };
+    const int nst = (nkeys + S::ROWS - 1) / S::ROWS;
+    if (nst > 0) dma_stage(0);
+    if (NBUF > 2 && nst > 1) dma_stage(1);
+
+    // ---- this lane's rows: row l32 of each of the wave's tiles
+    U4 qf[QT][KS];
+    long long row[QT];                                // row of the segment, -1: none
+    size_t at_q[QT];                                  // (query, head) of the tensor
+    bool takes[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        row[t] = blk * BM + (FEW ? 0 : wave * 32 * QT) + t * 32 + l32;
+        const int r = (int)min(row[t], rows - 1);     // past the end: the last row again, never stored
+        const int i = divide(r, a.G, a.by_g), g = r - i * a.G;
+        takes[t] = row[t] < live;
+        if (row[t] >= rows) row[t] = -1;
+        at_q[t] = (size_t)(qs.from + i) * a.H + kh * a.G + g;
+        const uint16_t* const from = a.q + at_q[t] * D + hf * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[t][ks].u = *reinterpret_cast<const uint4*>(from + ks * 16);
+    }
+    const bool busy = FEW || blk * BM + wave * 32 * QT < live;   // this wave has rows with results
+    if (!F16) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) qf[t][ks] = scale_pow2(qf[t][ks], a.q_pow2);
+        }
+    }
+    uint32_t koff[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) koff[ks] = sK + T::row_piece(lane, ks);
+    const uint32_t voff = sV + T::transposed(lane);
+    const float mul = a.s_mul;
+
+    f32x16 o[QT][MT];
+    float m[QT], l[QT];                               // reference of the exponentials (log2 units), their sum over this lane's keys
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        m[t] = -INFINITY;
+        l[t] = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) o[t][mt] = f32x16{0};
+    }
+
+    auto tile = [&](uint32_t at, int kbase) __attribute__((always_inline)) {
+        U4 kf[KS];
+        f32x16 s[QT];
+        U4 p0[QT], p1[QT];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[ks].u = lds_read16(koff[ks] + at);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            s[t] = f32x16{0};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s[t] = E::mfma(kf[ks], qf[t][ks], s[t]);
+        }
+        if (kbase + 32 > nkeys) {                     // the last tile may be short
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (kbase + 8 * (r >> 2) + 4 * hf + (r & 3) >= nkeys) s[t][r] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            float mx = fmaxf(fmaxf(s[t][0], s[t][1]), s[t][2]);
+#pragma unroll
+            for (int r = 3; r < 15; r += 2) mx = fmaxf(fmaxf(mx, s[t][r]), s[t][r + 1]);
+            mx = fmaxf(mx, s[t][15]);
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);   // the row's other keys
+            mx = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1])) * mul;
+            if (__builtin_amdgcn_ballot_w64(mx > m[t] + 8.0f)) {
+                const float top = fmaxf(m[t], mx), alpha = __builtin_amdgcn_exp2f(m[t] - top);   // the first time 2^-inf, onto zeros
+                m[t] = top;
+                l[t] *= alpha;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[t][mt][r] *= alpha;
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], mul, -m[t]));
+                l[t] += s[t][r];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                (&p0[t].u.x)[e] = E::pack(s[t][2 * e], s[t][2 * e + 1]);
+                (&p1[t].u.x)[e] = E::pack(s[t][8 + 2 * e], s[t][8 + 2 * e + 1]);
+            }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            U4 v0, v1;
+            read_transposed<D>(v0, v1, voff + at, (voff + at) ^ T::FLIP, mt);
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                o[t][mt] = E::mfma(v0, p0[t], o[t][mt]);
+                o[t][mt] = E::mfma(v1, p1[t], o[t][mt]);
+            }
+        }
+    };
+
+    for (int st = 0; st < nst; ++st) {
+        // this wave's loads of the stage are here: at most those of the next one are younger
+        if (NBUF > 2 && st + 1 < nst) __builtin_amdgcn_s_waitcnt(vm_wait(2 * LPW));
+        else __builtin_amdgcn_s_waitcnt(vm_wait(0));
+        __syncthreads();                              // every wave's are, and the buffer of stage st - 1 has been read
+        if (st + NBUF - 1 < nst) dma_stage(st + NBUF - 1);
+        if (!busy) continue;
+        const uint32_t at = (st % NBUF) * S::BYTES;
+        if (FEW) {
+            if (st * S::ROWS + wave * 32 < nkeys) tile(at + wave * T::BYTES, st * S::ROWS + wave * 32);
+        } else {
+#pragma unroll 1
+            for (int t4 = 0; t4 < S::TILES && st * S::ROWS + t4 * 32 < nkeys; ++t4) tile(at + t4 * T::BYTES, st * S::ROWS + t4 * 32);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(l[t]), __float_as_int(l[t]), false, false);
+        l[t] = __int_as_float(sw[0]) + __int_as_float(sw[1]);
+    }
+
+    if constexpr (FEW) {
+        // ---- the four waves' results meet in LDS: row by row, channels in order
+        constexpr int P = D + 4;                      // floats from one row to the next
+        static_assert(4 * 32 * P * 4 <= S::TOTAL, "room for the results");
+        float* const meet = reinterpret_cast<float*>(smem);
+        __shared__ float sm_[4][32], sl_[4][32];
+        __syncthreads();                              // the last stage has been read
+        if (hf == 0) {
+            sm_[wave][l32] = m[0];
+            sl_[wave][l32] = l[0];
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4)
+                *reinterpret_cast<float4*>(meet + (wave * 32 + l32) * P + mt * 32 + 8 * r4 + 4 * hf) =
+                    make_float4(o[0][mt][4 * r4], o[0][mt][4 * r4 + 1], o[0][mt][4 * r4 + 2], o[0][mt][4 * r4 + 3]);
+        }
+        __syncthreads();
+        constexpr int EACH = D / 8;                   // channels of a thread: eight of them to a row
+        const int rr = tid >> 3, c0 = (tid & 7) * EACH;
+        const long long r = blk * BM + rr;
+        if (r >= rows) return;
+        const int i = divide((int)r, a.G, a.by_g), g = (int)r - i * a.G;
+        const size_t at = (size_t)(qs.from + i) * a.H + kh * a.G + g;
+        const bool counts = r < live;
+        const float top = fmaxf(fmaxf(sm_[0][rr], sm_[1][rr]), fmaxf(sm_[2][rr], sm_[3][rr]));
+        float w[4], sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {                 // a wave without keys has -inf, and so has `top` where all have
+            w[k] = sm_[k][rr] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm_[k][rr] - top);
+            sum += w[k] * sl_[k][rr];
+        }
+        float y[EACH];
+#pragma unroll
+        for (int c = 0; c < EACH; ++c) {
+            y[c] = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (w[k] != 0.f) y[c] += w[k] * meet[(k * 32 + rr) * P + c0 + c];
+        }
+        if (!counts) sum = 0.f;
+        if (SPLIT) {
+            const size_t pa = (size_t)part * a.n_q * a.H + at;
+            if ((tid & 7) == 0) a.part_ml[pa] = make_float2(sum > 0.f ? top : -INFINITY, sum);
+            if (sum > 0.f) {
+#pragma unroll
+                for (int c = 0; c < EACH; c += 2) *reinterpret_cast<float2*>(a.part_o + pa * D + c0 + c) = make_float2(y[c], y[c + 1]);
+            }
+            return;
+        }
+        const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+        if (a.lse && (tid & 7) == 0) a.lse[at] = sum > 0.f ? (top + __log2f(sum)) * LN2 : -INFINITY;
+#pragma unroll
+        for (int c = 0; c < EACH; c += 2) {
+            const uint32_t pair = sum > 0.f ? E::pack(y[c] * inv, y[c + 1] * inv) : 0u;
+            *reinterpret_cast<uint32_t*>(a.out + at * D + c0 + c) = pair;
+        }
+        return;
+    }
+
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        if (row[t] < 0) continue;
+        const bool has = takes[t] && nkeys > 0;
+        if (SPLIT) {
+            const size_t pa = (size_t)part * a.n_q * a.H + at_q[t];
+            if (hf == 0) a.part_ml[pa] = has ? make_float2(m[t], l[t]) : make_float2(-INFINITY, 0.f);
+            if (!has) continue;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4)
+                    *reinterpret_cast<float4*>(a.part_o + pa * D + mt * 32 + 8 * r4 + 4 * hf) =
+                        make_float4(o[t][mt][4 * r4], o[t][mt][4 * r4 + 1], o[t][mt][4 * r4 + 2], o[t][mt][4 * r4 + 3]);
+            }
+            continue;
+        }
+        const float inv = 1.0f / l[t];
+        if (a.lse && hf == 0) a.lse[at_q[t]] = has ? (m[t] + __log2f(l[t])) * LN2 : -INFINITY;
+        uint16_t* const to = a.out + at_q[t] * D;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4) {
+                uint2 y = make_uint2(0, 0);
+                if (has) {
+                    y.x = E::pack(o[t][mt][4 * r4] * inv, o[t][mt][4 * r4 + 1] * inv);
+                    y.y = E::pack(o[t][mt][4 * r4 + 2] * inv, o[t][mt][4 * r4 + 3] * inv);
+                }
+                *reinterpret_cast<uint2*>(to + mt * 32 + 8 * r4 + 4 * hf) = y;
+            }
+        }
+    }
+}
+
+// The parts of every (row, head): D / 4 threads, four channels each
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void k_cross_join(CrossArgs a)
+{
+    constexpr int TPR = D / 4;
+    const long long n = (long long)a.n_q * a.H, at = (long long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    const int c = (threadIdx.x % TPR) * 4;
+    if (at >= n) return;
+    // rows behind the last segment, or before the first, belong to nobody: they stay as they were
+    const long long q = at / a.H;
+    if (q < offset_of(a.q_offsets, a.n_q, 0) || q >= offset_of(a.q_offsets, a.n_q, a.segments)) return;
+    float top = -INFINITY;
+    for (int p = 0; p < a.parts; ++p) top = fmaxf(top, a.part_ml[p * n + at].x);
+    float sum = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int p = 0; p < a.parts; ++p) {
+        const float2 ml = a.part_ml[p * n + at];
+        if (ml.x == -INFINITY) continue;              // no keys in this part: nothing was stored
+        const float w = __builtin_amdgcn_exp2f(ml.x - top);
+        const float4 o = *reinterpret_cast<const float4*>(a.part_o + (p * n + at) * D + c);
+        sum += w * ml.y;
+        y[0] += w * o.x;
+        y[1] += w * o.y;
+        y[2] += w * o.z;
+        y[3] += w * o.w;
+    }
+    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+    if (a.lse && c == 0) a.lse[at] = sum > 0.f ? (top + __log2f(sum)) * LN2 : -INFINITY;
+    *reinterpret_cast<uint2*>(a.out + at * D + c) =
+        make_uint2(Half<F16>::pack(y[0] * inv, y[1] * inv), Half<F16>::pack(y[2] * inv, y[3] * inv));
+}
+
+template <int D, bool F16>
+hipError_t launch(const CrossArgs& a, hipStream_t stream)
+{
+    const long long total = ((long long)a.slots * a.K * a.parts + 7) / 8 * 8;
+    const unsigned grid = (unsigned)total;
+    constexpr int QT2 = D <= 64 ? 2 : 1;
+    const bool split = a.parts > 1;
+    if (a.few) {
+        if (split) k_cross<D, 1, true, F16, true><<<grid, 256, 0, stream>>>(a);
+        else k_cross<D, 1, true, F16, false><<<grid, 256, 0, stream>>>(a);
+    } else if (a.row_tiles == 2) {
+        if (split) return hipErrorInvalidValue;       // two tiles a wave are for launches that fill the chip
+        k_cross<D, QT2, false, F16, false><<<grid, 256, 0, stream>>>(a);
+    } else {
+        if (split) k_cross<D, 1, false, F16, true><<<grid, 256, 0, stream>>>(a);
+        else k_cross<D, 1, false, F16, false><<<grid, 256, 0, stream>>>(a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !split) return e;
+    constexpr int PER = 256 / (D / 4);
+    k_cross_join<D, F16><<<(unsigned)(((long long)a.n_q * a.H + PER - 1) / PER), 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_typed(const CrossArgs& a, hipStream_t stream)
+{
+    return a.f16 ? launch<D, true>(a, stream) : launch<D, false>(a, stream);
+}
+
+}  // namespace
+
+CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_q, long long max_kv, int heads, int kv_heads, int head_dim, bool backward)
+{
+    constexpr long long CUS = 256;
+    const int group = heads / kv_heads;
+    CrossPlan p = {};
+    const long long rows = n_q * group;               // of one key/value head
+    p.few = max_q * group <= 32 && !backward;
+    p.row_tiles = !p.few && head_dim <= (backward ? 32 : 64) && (rows / 256) * kv_heads >= 2 * CUS ? 2 : 1;
+    const int block = p.few ? 32 : 128 * p.row_tiles;
+    p.slots = (int)(rows / block + segments);
+    // fewer than two workgroups per compute unit: parts of 256 keys at least, until there are about three
+    const long long work = (rows + block - 1) / block < 1 ? 1 : (rows + block - 1) / block;
+    const long long blocks = (work > segments ? work : segments) * kv_heads;
+    long long parts = 1;
+    if (p.row_tiles == 1 && blocks < 2 * CUS) {
+        parts = (3 * CUS + blocks - 1) / blocks;
+        const long long most = (max_kv + 255) / 256;
+        if (parts > most) parts = most;
+        if (parts < 1) parts = 1;
+    }
+    p.chunk = (int)(((max_kv + parts - 1) / parts + 127) / 128 * 128);
+    if (p.chunk < 128) p.chunk = 128;
+    p.parts = (int)((max_kv + p.chunk - 1) / p.chunk);
+    if (p.parts < 1) p.parts = 1;
+    if (!backward) return p;
+    p.kv_slots = (int)(n_kv / 128 + segments);
+    const long long kv_work = n_kv / 128 > segments ? n_kv / 128 : segments;
+    long long row_parts = 1;
+    if (kv_work * kv_heads < 2 * CUS) {
+        row_parts = (3 * CUS + kv_work * kv_heads - 1) / (kv_work * kv_heads);
+        const long long most = (max_q * group + 255) / 256;
+        if (row_parts > most) row_parts = most;
+        if (row_parts < 1) row_parts = 1;
+    }
+    const long long chunk = ((max_q * group + row_parts - 1) / row_parts + 127) / 128 * 128;
+    p.row_chunk = (int)(chunk < 128 ? 128 : chunk);
+    p.row_parts = (int)((max_q * group + p.row_chunk - 1) / p.row_chunk);
+    if (p.row_parts < 1) p.row_parts = 1;
+    return p;
+}
+
+hipError_t cross_launch(const CrossArgs& a, int head_dim, hipStream_t stream)
+{
+    switch (head_dim) {
+        case 16: return launch_typed<16>(a, stream);
+        case 32: return launch_typed<32>(a, stream);
+        case 64: return launch_typed<64>(a, stream);
+        case 128: return launch_typed<128>(a, stream);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+}  // namespace f3d

@@ -1,0 +1,448 @@
+// Cross attention backward for gfx950.
+//
+//   P = exp(S - lse),  dP = dO v^T,  D_i = sum_c dO_ic O_ic,  dS = P o (dP - D),
+//   dq = scale dS k,  dk = scale dS^T q,  dv = P^T dO,  the last two summed over the heads that share the key/value head
+//
+// Two kernels, as for the attention inside scopes, and neither needs atomics:
+//   k_cross_bwd_dq    owns query rows, streams K and V, works out D on the way. Scores are computed transposed (keys x rows), so a lane
+//                     owns 16 keys of ONE row: lse and D are per-lane scalars, and dS^T, packed to bf16, is the B operand of
+//                     dQ^T += K^T dS^T.
+//   k_cross_bwd_dkdv  owns 128 keys of a key/value head, streams the rows of all heads that share it (after the first kernel: it reads
+//                     D). Scores are rows x keys, a lane owns 16 rows of ONE key; P and dS are the B operands of dV^T += dO^T P and
+//                     dK^T += Q^T dS. The sum over shared heads is the sum over rows.
+// Few keys beside many rows (or the reverse) leave one of the two with a handful of workgroups: then its sum over rows (over keys) is split
+// into parts, kept in binary32 and added up in a fixed order by a last kernel.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "cross_common.h"
+
+namespace f3d {
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+template <int D>
+struct BStage {
+    using T = Tile<D>;
+    static constexpr int ROWS = D == 128 ? 64 : 128;
+    static constexpr int TILES = ROWS / 32;
+    static constexpr int BYTES = ROWS * T::ROWB;      // of one operand
+    static constexpr int NBUF = 2;
+    static constexpr int LPW = ROWS * T::NC / 256;
+    static constexpr int TOTAL = NBUF * 2 * BYTES;
+};
+
+__device__ __forceinline__ f32x16 mfma(const U4& x, const U4& y, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.b, y.b, c, 0, 0, 0);
+}
+
+// 32 channels of a result's row from the lane that owns it, in binary32 (`part`) or rounded
+template <int D, int MT>
+__device__ __forceinline__ void store_row(float* part, uint16_t* to, const f32x16 (&acc)[MT], int hf, float mul, bool has)
+{
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4) {
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (has) y = make_float4(acc[mt][4 * r4] * mul, acc[mt][4 * r4 + 1] * mul, acc[mt][4 * r4 + 2] * mul, acc[mt][4 * r4 + 3] * mul);
+            const int c = mt * 32 + 8 * r4 + 4 * hf;
+            if (part) *reinterpret_cast<float4*>(part + c) = y;
+            else *reinterpret_cast<uint2*>(to + c) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+        }
+    }
+}
+
+// Rows of a tensor that no segment owns get zeros from all workgroups of a launch together; there are none as a rule
+__device__ __forceinline__ void zero_rest(const int32_t* offsets, int segments, int n, uint32_t row_bytes, uint16_t* x, uint16_t* y)
+{
+    const int before = offset_of(offsets, n, 0), from = offset_of(offsets, n, segments);
+    if (before == 0 && from == n) return;
+    const long long head = (long long)min(before, from) * row_bytes / 16, tail = (long long)from * row_bytes / 16, all = (long long)n * row_bytes / 16;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < head + all - tail; i += (long long)gridDim.x * 256) {
+        const long long at = i < head ? i : tail + (i - head);
+        reinterpret_cast<uint4*>(x)[at] = make_uint4(0, 0, 0, 0);
+        if (y) reinterpret_cast<uint4*>(y)[at] = make_uint4(0, 0, 0, 0);
+    }
+}
+
+template <int D, int QT, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void k_cross_bwd_dq(CrossBwdArgs b)
+{
+    using T = Tile<D>;
+    using S = BStage<D>;
+    constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF;
+    constexpr int BM = 128 * QT, SHIFT = QT == 2 ? 8 : 7;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[S::TOTAL];
+    const CrossArgs& a = b.f;
+    const uint32_t sK = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sV = sK + NBUF * S::BYTES;
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (!SPLIT) zero_rest(a.q_offsets, a.segments, a.n_q, (uint32_t)a.H * T::ROWB, b.dq, nullptr);
+    const uint32_t u = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);   // as in the forward kernel
+    const uint32_t x = u / (uint32_t)a.K;
+    const int kh = (int)(u - x * a.K), slot = (int)(SPLIT ? x / (uint32_t)a.parts : x), part = SPLIT ? (int)(x - (uint32_t)slot * a.parts) : 0;
+    if (slot >= a.slots) return;
+    const int seg = segment_of(a.q_offsets, a.n_q, a.segments, a.G, SHIFT, slot);
+    const Rows qs = rows_of(a.q_offsets, a.q_lens, a.n_q, seg), kv = rows_of(a.kv_offsets, a.kv_lens, a.n_kv, seg);
+    const long long blk = slot - first_slot(a.q_offsets, a.n_q, seg, a.G, SHIFT);
+    const long long rows = (long long)qs.span * a.G, live = (long long)qs.len * a.G;
+    if (blk < 0 || blk * BM >= rows) return;
+    const int key0 = SPLIT ? part * a.chunk : 0;
+    const int nkeys = blk * BM >= live ? 0 : SPLIT ? min(max(kv.len - key0, 0), a.chunk) : kv.len;
+
+    const uint32_t row_bytes = (uint32_t)a.K * T::ROWB;
+    const uint64_t first = (uint64_t)(kv.from + key0) * row_bytes + (uint64_t)kh * T::ROWB;
+    int srow[LPW];
+    uint32_t scol[LPW];
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+        const int p = (wave * LPW + i) * 64 + lane;
+        srow[i] = p / T::NC;
+        scol[i] = ((p % T::NC) ^ T::swizzle(srow[i])) << 4;
+    }
+    auto dma_stage = [&](int st) __attribute__((always_inline)) {
+        const uint32_t to = (st % NBUF) * S::BYTES;
+#pragma unroll
+        for (int i = 0; i < LPW; ++i) {
+            const int key = min(st * S::ROWS + srow[i], nkeys - 1);
+            const uint64_t at = first + (uint64_t)(uint32_t)key * row_bytes + scol[i];
+            lds_dma16(reinterpret_cast<const char*>(a.k) + at, sK + to + (wave * LPW + i) * 1024);
+            lds_dma16(reinterpret_cast<const char*>(a.v) + at, sV + to + (wave * LPW + i) * 1024);
+        }
+    };
+    const int nst = (nkeys + S::ROWS - 1) / S::ROWS;
+    if (nst > 0) dma_stage(0);
+
+    U4 qf[QT][KS], gf[QT][KS];
+    long long row[QT];
+    size_t at_q[QT];
+    bool takes[QT];
+    float nl[QT], dsum[QT];
+    f32x16 acc[QT][MT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        row[t] = blk * BM + wave * 32 * QT + t * 32 + l32;
+        const int r = (int)min(row[t], max(live, 1ll) - 1);   // past the end, or behind the segment's length: a row that counts, dropped
+        const int i = divide(r, a.G, a.by_g), g = r - i * a.G;
+        const size_t at = (size_t)(qs.from + i) * a.H + kh * a.G + g;
+        takes[t] = row[t] < live;
+        const int ro = (int)min(row[t], rows - 1), io = divide(ro, a.G, a.by_g);
+        at_q[t] = (size_t)(qs.from + io) * a.H + kh * a.G + (ro - io * a.G);
+        if (row[t] >= rows) row[t] = -1;
+        float dot = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            U4 of;
+            const size_t from = at * D + ks * 16 + hf * 8;
+            qf[t][ks].u = *reinterpret_cast<const uint4*>(a.q + from);
+            gf[t][ks].u = *reinterpret_cast<const uint4*>(b.dout + from);
+            of.u = *reinterpret_cast<const uint4*>(a.out + from);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t y = (&of.u.x)[e], z = (&gf[t][ks].u.x)[e];
+                dot += __uint_as_float(y << 16) * __uint_as_float(z << 16);
+                dot += __uint_as_float(y & 0xFFFF0000u) * __uint_as_float(z & 0xFFFF0000u);
+            }
+            qf[t][ks] = scale_pow2(qf[t][ks], a.q_pow2);
+        }
+        dsum[t] = dot + __shfl_xor(dot, 32, 64);
+        if (takes[t] && part == 0 && hf == 0) b.dsum[at] = dsum[t];
+        nl[t] = takes[t] && nkeys > 0 ? -LOG2E * a.lse[at] : -1e30f;   // rows that take no part: probabilities exactly zero
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) acc[t][mt] = f32x16{0};
+    }
+    const bool busy = blk * BM + wave * 32 * QT < live;
+    uint32_t off[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) off[ks] = T::row_piece(lane, ks);
+    const uint32_t toff = sK + T::transposed(lane);
+    const float mul = a.s_mul;
+
+    auto tile = [&](uint32_t at, int kbase) __attribute__((always_inline)) {
+        U4 kf[KS], vf[KS];
+        f32x16 s[QT], dp[QT];
+        U4 p0[QT], p1[QT];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            kf[ks].u = lds_read16(sK + at + off[ks]);
+            vf[ks].u = lds_read16(sV + at + off[ks]);
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            s[t] = f32x16{0};
+            dp[t] = f32x16{0};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s[t] = mfma(kf[ks], qf[t][ks], s[t]);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) dp[t] = mfma(vf[ks], gf[t][ks], dp[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dp[t][r] = (dp[t][r] - dsum[t]) * __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], mul, nl[t]));
+            if (kbase + 32 > nkeys) {                 // keys past the end repeat one: their dS is dropped
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (kbase + 8 * (r >> 2) + 4 * hf + (r & 3) >= nkeys) dp[t][r] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                (&p0[t].u.x)[e] = pack_bf16(dp[t][2 * e], dp[t][2 * e + 1]);
+                (&p1[t].u.x)[e] = pack_bf16(dp[t][8 + 2 * e], dp[t][8 + 2 * e + 1]);
+            }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            U4 k0, k1;
+            read_transposed<D>(k0, k1, toff + at, (toff + at) ^ T::FLIP, mt);
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                acc[t][mt] = mfma(k0, p0[t], acc[t][mt]);
+                acc[t][mt] = mfma(k1, p1[t], acc[t][mt]);
+            }
+        }
+    };
+    for (int st = 0; st < nst; ++st) {
+        __builtin_amdgcn_s_waitcnt(vm_wait(0));       // this wave's loads of the stage are here
+        __syncthreads();                              // every wave's are, and the other buffer has been read
+        if (st + 1 < nst) dma_stage(st + 1);
+        if (!busy) continue;
+        const uint32_t at = (st % NBUF) * S::BYTES;
+#pragma unroll 1
+        for (int t4 = 0; t4 < S::TILES && st * S::ROWS + t4 * 32 < nkeys; ++t4) tile(at + t4 * T::BYTES, st * S::ROWS + t4 * 32);
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        if (row[t] < 0) continue;
+        float* const p = SPLIT ? b.part_dq + ((size_t)part * a.n_q * a.H + at_q[t]) * D : nullptr;
+        store_row<D, MT>(p, b.dq + at_q[t] * D, acc[t], hf, b.scale, takes[t] && nkeys > 0);
+    }
+}
+
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossBwdArgs b)
+{
+    using T = Tile<D>;
+    using S = BStage<D>;
+    constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF, BM = 128, SHIFT = 7;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[S::TOTAL];
+    __shared__ __attribute__((aligned(16))) float sl[NBUF][S::ROWS], sd[NBUF][S::ROWS];   // -lse (log2 units) and D of the staged rows
+    const CrossArgs& a = b.f;
+    const uint32_t sQ = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sG = sQ + NBUF * S::BYTES;
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (!SPLIT) zero_rest(a.kv_offsets, a.segments, a.n_kv, (uint32_t)a.K * T::ROWB, b.dk, b.dv);
+    const uint32_t u = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    const uint32_t x = u / (uint32_t)a.K;
+    const int kh = (int)(u - x * a.K), slot = (int)(SPLIT ? x / (uint32_t)b.row_parts : x), part = SPLIT ? (int)(x - (uint32_t)slot * b.row_parts) : 0;
+    if (slot >= b.kv_slots) return;
+    const int seg = segment_of(a.kv_offsets, a.n_kv, a.segments, 1, SHIFT, slot);
+    const Rows qs = rows_of(a.q_offsets, a.q_lens, a.n_q, seg), kv = rows_of(a.kv_offsets, a.kv_lens, a.n_kv, seg);
+    const long long blk = slot - first_slot(a.kv_offsets, a.n_kv, seg, 1, SHIFT);
+    if (blk < 0 || blk * BM >= kv.span) return;
+    const int row0 = SPLIT ? part * b.row_chunk : 0, live = qs.len * a.G;
+    const int nrows = blk * BM >= kv.len ? 0 : SPLIT ? min(max(live - row0, 0), b.row_chunk) : live;
+
+    const uint32_t row_bytes = (uint32_t)a.H * T::ROWB;
+    int srow[LPW];
+    uint32_t scol[LPW];
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+        const int p = (wave * LPW + i) * 64 + lane;
+        srow[i] = p / T::NC;
+        scol[i] = ((p % T::NC) ^ T::swizzle(srow[i])) << 4;
+    }
+    float nl = 0.f, ds = 0.f;                         // of row `tid` of the stage requested last
+    auto dma_stage = [&](int st) __attribute__((always_inline)) {
+        const uint32_t to = (st % NBUF) * S::BYTES;
+#pragma unroll
+        for (int i = 0; i < LPW; ++i) {
+            const int r = row0 + min(st * S::ROWS + srow[i], nrows - 1);
+            const int q = divide(r, a.G, a.by_g), g = r - q * a.G;
+            const uint64_t at = (uint64_t)(qs.from + q) * row_bytes + (uint32_t)(kh * a.G + g) * T::ROWB + scol[i];
+            lds_dma16(reinterpret_cast<const char*>(a.q) + at, sQ + to + (wave * LPW + i) * 1024);
+            lds_dma16(reinterpret_cast<const char*>(b.dout) + at, sG + to + (wave * LPW + i) * 1024);
+        }
+        if (tid < S::ROWS) {
+            const int r = st * S::ROWS + tid, rc = row0 + min(r, nrows - 1);
+            const int q = divide(rc, a.G, a.by_g), g = rc - q * a.G;
+            const size_t at = (size_t)(qs.from + q) * a.H + kh * a.G + g;
+            const float l = a.lse[at], d = b.dsum[at];
+            nl = r < nrows ? -LOG2E * l : -1e30f;     // past the end: probabilities exactly zero
+            ds = d;
+        }
+    };
+    auto keep_sums = [&](int st) __attribute__((always_inline)) {
+        if (tid < S::ROWS) {
+            sl[st % NBUF][tid] = nl;
+            sd[st % NBUF][tid] = ds;
+        }
+    };
+    const int nst = (nrows + S::ROWS - 1) / S::ROWS;
+    if (nst > 0) dma_stage(0);
+
+    const long long key = blk * BM + wave * 32 + l32;
+    const bool has = key < kv.len && nrows > 0;
+    const bool busy = blk * BM + wave * 32 < kv.len;
+    U4 kf[KS], vf[KS];
+    f32x16 dk[MT], dv[MT];
+    {
+        const size_t at = ((size_t)(kv.from + min(key, (long long)max(kv.len, 1) - 1)) * a.K + kh) * D + hf * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            kf[ks].u = *reinterpret_cast<const uint4*>(a.k + at + ks * 16);
+            vf[ks].u = *reinterpret_cast<const uint4*>(a.v + at + ks * 16);
+            kf[ks] = scale_pow2(kf[ks], a.q_pow2);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) dk[mt] = dv[mt] = f32x16{0};
+    }
+    uint32_t off[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) off[ks] = T::row_piece(lane, ks);
+    const uint32_t tr = T::transposed(lane);
+    const float mul = a.s_mul;
+    if (nst > 0) keep_sums(0);
+
+    auto tile = [&](int buf, int t4) __attribute__((always_inline)) {
+        const uint32_t at = buf * S::BYTES + t4 * T::BYTES;
+        f32x16 s = f32x16{0}, dp = f32x16{0};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            U4 qf, gf;
+            qf.u = lds_read16(sQ + at + off[ks]);
+            gf.u = lds_read16(sG + at + off[ks]);
+            s = mfma(qf, kf[ks], s);
+            dp = mfma(gf, vf[ks], dp);
+        }
+        U4 p0, p1, d0, d1;
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+            const float4 l = *reinterpret_cast<const float4*>(&sl[buf][t4 * 32 + 8 * r4 + 4 * hf]);
+            const float4 d = *reinterpret_cast<const float4*>(&sd[buf][t4 * 32 + 8 * r4 + 4 * hf]);
+            const float lv[4] = {l.x, l.y, l.z, l.w}, dd[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 4 * r4 + e;
+                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], mul, lv[e]));
+                dp[r] = (dp[r] - dd[e]) * s[r];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            (&p0.u.x)[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
+            (&p1.u.x)[e] = pack_bf16(s[8 + 2 * e], s[8 + 2 * e + 1]);
+            (&d0.u.x)[e] = pack_bf16(dp[2 * e], dp[2 * e + 1]);
+            (&d1.u.x)[e] = pack_bf16(dp[8 + 2 * e], dp[8 + 2 * e + 1]);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            U4 g0, g1, q0, q1;
+            read_transposed<D>(g0, g1, sG + at + tr, (sG + at + tr) ^ T::FLIP, mt);
+            read_transposed<D>(q0, q1, sQ + at + tr, (sQ + at + tr) ^ T::FLIP, mt);
+            dv[mt] = mfma(g0, p0, dv[mt]);
+            dk[mt] = mfma(q0, d0, dk[mt]);
+            dv[mt] = mfma(g1, p1, dv[mt]);
+            dk[mt] = mfma(q1, d1, dk[mt]);
+        }
+    };
+    for (int st = 0; st < nst; ++st) {
+        __builtin_amdgcn_s_waitcnt(vm_wait(0));
+        __syncthreads();
+        if (st + 1 < nst) dma_stage(st + 1);
+        if (busy) {
+#pragma unroll 1
+            for (int t4 = 0; t4 < S::TILES && st * S::ROWS + t4 * 32 < nrows; ++t4) tile(st % NBUF, t4);
+        }
+        if (st + 1 < nst) keep_sums(st + 1);          // its buffer was read before the barrier above
+    }
+    if (key >= kv.span) return;
+    const size_t at = ((size_t)(kv.from + key) * a.K + kh) * D, all = (size_t)a.n_kv * a.K * D;
+    float* const p = SPLIT ? b.part_dkv + part * all + at : nullptr;
+    store_row<D, MT>(p, b.dk + at, dk, hf, b.scale, has);
+    store_row<D, MT>(SPLIT ? p + b.row_parts * all : nullptr, b.dv + at, dv, hf, 1.0f, has);
+}
+
+// The parts of a gradient, four channels a thread; rows that no segment owns get zeros. y: a second gradient, whose parts follow
+__global__ __launch_bounds__(256) void k_cross_bwd_join(const float* part, int parts, long long n, int row_pieces, const int32_t* offsets,
+                                                        int segments, int n_rows, uint16_t* x, uint16_t* y)
+{
+    long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    uint16_t* to = x;
+    if (i >= n) {
+        if (!y || i >= 2 * n) return;
+        i -= n;
+        to = y;
+        part += (size_t)parts * n * 4;
+    }
+    const long long row = i / row_pieces;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (row >= offset_of(offsets, n_rows, 0) && row < offset_of(offsets, n_rows, segments)) {
+#pragma unroll 4
+        for (int p = 0; p < parts; ++p) {
+            const float4 f = reinterpret_cast<const float4*>(part)[p * n + i];
+            s.x += f.x;
+            s.y += f.y;
+            s.z += f.z;
+            s.w += f.w;
+        }
+    }
+    reinterpret_cast<uint2*>(to)[i] = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
+}
+
+template <int D>
+hipError_t launch(const CrossBwdArgs& b, hipStream_t stream)
+{
+    const CrossArgs& a = b.f;
+    hipError_t e;
+    if (a.n_q > 0) {
+        const unsigned grid = (unsigned)(((long long)a.slots * a.K * a.parts + 7) / 8 * 8);
+        constexpr int QT2 = D <= 32 ? 2 : 1;
+        if (a.parts > 1) k_cross_bwd_dq<D, 1, true><<<grid, 256, 0, stream>>>(b);
+        else if (a.row_tiles == 2) k_cross_bwd_dq<D, QT2, false><<<grid, 256, 0, stream>>>(b);
+        else k_cross_bwd_dq<D, 1, false><<<grid, 256, 0, stream>>>(b);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (a.parts > 1) {
+            const long long n = (long long)a.n_q * a.H * (D / 4);
+            k_cross_bwd_join<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(b.part_dq, a.parts, n, a.H * (D / 4), a.q_offsets, a.segments, a.n_q,
+                                                                           b.dq, nullptr);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+    }
+    if (a.n_kv > 0) {
+        const unsigned grid = (unsigned)(((long long)b.kv_slots * a.K * b.row_parts + 7) / 8 * 8);
+        if (b.row_parts > 1) k_cross_bwd_dkdv<D, true><<<grid, 256, 0, stream>>>(b);
+        else k_cross_bwd_dkdv<D, false><<<grid, 256, 0, stream>>>(b);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (b.row_parts > 1) {
+            const long long n = (long long)a.n_kv * a.K * (D / 4);
+            k_cross_bwd_join<<<(unsigned)((2 * n + 255) / 256), 256, 0, stream>>>(b.part_dkv, b.row_parts, n, a.K * (D / 4), a.kv_offsets,
+                                                                               a.segments, a.n_kv, b.dk, b.dv);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t cross_bwd_launch(const CrossBwdArgs& b, int head_dim, hipStream_t stream)
+{
+    switch (head_dim) {
+        case 16: return launch<16>(b, stream);
+        case 32: return launch<32>(b, stream);
+        case 64: return launch<64>(b, stream);
+        case 128: return launch<128>(b, stream);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+}  // namespace f3d

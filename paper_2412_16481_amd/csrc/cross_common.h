@@ -1,0 +1,122 @@
+// Device helpers shared by the cross attention's forward (cross.hip) and backward (cross_bwd.hip): segments and their rows, the
+// layout of staged rows in LDS, 16-bit element types.
+#pragma once
+#include "attn_common.h"
+#include "cross.h"
+
+namespace f3d {
+
+namespace {
+
+template <bool F16>
+struct Half {
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi)
+    {
+        if constexpr (F16) {
+            const f32x2 x = {lo, hi};
+            const f16x2 y = __builtin_convertvector(x, f16x2);   // round to nearest even
+            return *reinterpret_cast<const uint32_t*>(&y);
+        } else {
+            return pack_bf16(lo, hi);
+        }
+    }
+    static __device__ __forceinline__ f32x16 mfma(const U4& x, const U4& y, f32x16 c)
+    {
+        if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(x.f, y.f, c, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.b, y.b, c, 0, 0, 0);
+    }
+};
+
+// A segment's rows in a tensor of n: [from, from + span), of which the first `len` take part. Whatever the arrays hold, the rows
+// are the tensor's.
+struct Rows {
+    int from, span, len;
+};
+
+// first row of segment b; no offsets: one segment of all rows
+__device__ __forceinline__ int offset_of(const int32_t* offsets, int n, int b) { return offsets ? min(max(offsets[b], 0), n) : b ? n : 0; }
+
+__device__ __forceinline__ Rows rows_of(const int32_t* offsets, const int32_t* lens, int n, int b)
+{
+    Rows r;
+    r.from = offset_of(offsets, n, b);
+    r.span = max(offset_of(offsets, n, b + 1) - r.from, 0);
+    r.len = lens ? min(max(lens[b], 0), r.span) : r.span;
+    return r;
+}
+
+// Row blocks: segment b owns the block slots from first_slot(b) on; a block is 2^shift rows, a row of the tensor counts `per` times
+// (once per head that shares keys). floor((o + len) / B) - floor(o / B) + 1 is room for ceil(len / B) blocks wherever o is, so
+// neither the host nor another segment has to know how many there are.
+__device__ __forceinline__ long long first_slot(const int32_t* offsets, int n, int b, int per, int shift)
+{
+    return ((long long)offset_of(offsets, n, b) * per >> shift) + b;
+}
+
+// The segment that owns the slot, 64 candidates at a time: the last whose slots begin at or before it
+__device__ __forceinline__ int segment_of(const int32_t* offsets, int n, int segments, int per, int shift, int slot)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, left = segments;
+    while (left > 1) {
+        const int step = (left + 63) / 64, i = lane * step;
+        const bool before = i < left && first_slot(offsets, n, lo + min(i, left - 1), per, shift) <= slot;
+        // as a signed number: none begins before a slot in front of the first segment
+        const int owned = (int)__popcll(__builtin_amdgcn_ballot_w64(before)), k = owned > 0 ? owned - 1 : 0;
+        lo += k * step;
+        left = min(step, left - k * step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Rows of one head in LDS: row-major, the 16-byte pieces of a row xor-swizzled by the row, so that neither 16 rows read at one
+// piece nor the four rows x 64 bytes of a transposing read meet in a bank (256 bytes of them).
+template <int D>
+struct Tile {
+    static constexpr int NC = D / 8;              // 16-byte pieces of a row
+    static constexpr int ROWB = D * 2;            // bytes of a row
+    static constexpr int BYTES = 32 * ROWB;       // of a tile of 32 rows
+    static constexpr int KS = D / 16;             // steps of a product over the channels
+    static constexpr int MT = D <= 32 ? 1 : D / 32;   // blocks of 32 channels
+    static __device__ __forceinline__ int swizzle(int row)
+    {
+        if (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+        if (D == 64) return ((row & 2) << 1) | ((row >> 2) & 3);
+        if (D == 32) return (row >> 2) & 3;
+        return (row >> 3) & 1;
+    }
+    // byte offset of channels 16 ks + 8 hf .. of row l32: an operand whose rows are the tile's
+    static __device__ __forceinline__ uint32_t row_piece(int lane, int ks)
+    {
+        const int l32 = lane & 31, hf = lane >> 5;
+        return l32 * ROWB + (((2 * ks + hf) ^ swizzle(l32)) << 4);
+    }
+    // The transposing read that delivers X^T (rows: channels, k: the tile's rows in the order of the score registers). In a group
+    // of 16 lanes lane 4 j + c hands in the address of channels 4 c .. 4 c + 3 of row 4 hf + j, and of rows 8, 16, 24 further on: the
+    // swizzle of a row 8 further on differs in one bit, 16 further on it is the same. At 16 channels the second group of 16
+    // lanes repeats the first: the result rows it feeds are never read.
+    static __device__ __forceinline__ uint32_t transposed(int lane)
+    {
+        const int i16 = lane & 15, j = i16 >> 2, c = i16 & 3, g16 = (lane >> 4) & 1, hf = lane >> 5;
+        const int row = 4 * hf + j, piece = (D == 16 ? 0 : 2 * g16) + (c >> 1);
+        return row * ROWB + ((piece ^ swizzle(row)) << 4) + (c & 1) * 8;
+    }
+    static constexpr uint32_t FLIP = D == 16 ? 16 : 32;   // of the address, for rows 8 and 24 further on
+};
+
+// X^T of channels 32 mt .. of the tile whose transposed() address is `at` (with `flip` = at ^ FLIP)
+template <int D>
+__device__ __forceinline__ void read_transposed(U4& x0, U4& x1, uint32_t at, uint32_t flip, int mt)
+{
+    constexpr int STEP = 8 * Tile<D>::ROWB;
+    const uint32_t a = at ^ (mt * 64), f = flip ^ (mt * 64);
+    const uint2 y0 = lds_read_tr(a), y1 = lds_read_tr(f + STEP), y2 = lds_read_tr(a + 2 * STEP), y3 = lds_read_tr(f + 3 * STEP);
+    x0.u = make_uint4(y0.x, y0.y, y1.x, y1.y);
+    x1.u = make_uint4(y2.x, y2.y, y3.x, y3.y);
+}
+
+constexpr int vm_wait(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }   // s_waitcnt operand: the memory counter alone
+
+}  // namespace
+
+}  // namespace f3d

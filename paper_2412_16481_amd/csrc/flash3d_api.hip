@@ -12,6 +12,7 @@
 
 #include "attn.h"
 #include "clip.h"
+#include "cross.h"
 #include "flash3d.h"
 #include "linear.h"
 #include "norm.h"
@@ -624,6 +625,206 @@ int f3d_bucket_swin_attn_bwd(const void* q, const void* k, const void* v, const 
     set_divides(b.f);
     (void)hipGetLastError();
     const hipError_t e = f3d::attn_bwd_launch(b, head_dim, (hipStream_t)stream);
+    return e == hipSuccess ? F3D_OK : hip_fail(e);
+}
+
+// checks and launch geometry shared by the cross attention calls
+struct CrossSizes {
+    int64_t n_q, n_kv, max_q, max_kv;
+    int32_t n_segments, heads, kv_heads, head_dim;
+};
+
+static int cross_sizes(CrossSizes& s, int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q, int64_t max_kv, int32_t heads,
+                       int32_t kv_heads, int32_t head_dim)
+{
+    if (n_q < 0 || n_kv < 0 || n_segments < 1 || max_q < 0 || max_kv < 0 || heads < 1 || kv_heads < 1) return F3D_ERR_INVALID_ARG;
+    if (heads % kv_heads != 0) return F3D_ERR_INVALID_ARG;
+    if (head_dim != 16 && head_dim != 32 && head_dim != 64 && head_dim != 128) return F3D_ERR_UNSUPPORTED;
+    const int64_t most = (int64_t)2147483647 - (1 << 20);
+    if (n_segments > 65535 || (int64_t)heads * head_dim > 65536) return F3D_ERR_UNSUPPORTED;
+    if (n_q >= most / heads || n_kv >= most / kv_heads) return F3D_ERR_UNSUPPORTED;
+    s = {n_q, n_kv, max_q > 0 && max_q < n_q ? max_q : n_q, max_kv > 0 && max_kv < n_kv ? max_kv : n_kv, n_segments, heads, kv_heads, head_dim};
+    return F3D_OK;
+}
+
+static size_t cross_part_bytes(const CrossSizes& s, const f3d::CrossPlan& p)
+{
+    return p.parts > 1 ? align_up((size_t)p.parts * s.n_q * s.heads * s.head_dim * sizeof(float), 256) : 0;
+}
+
+static size_t cross_ml_bytes(const CrossSizes& s, const f3d::CrossPlan& p)
+{
+    return p.parts > 1 ? align_up((size_t)p.parts * s.n_q * s.heads * sizeof(float2), 256) : 0;
+}
+
+static f3d::CrossPlan cross_plan(const CrossSizes& s, bool backward)
+{
+    return f3d::cross_plan(s.n_q, s.n_kv, s.n_segments, s.max_q, s.max_kv, s.heads, s.kv_heads, s.head_dim, backward);
+}
+
+static int fill_cross_args(f3d::CrossArgs& a, const CrossSizes& s, const f3d::CrossPlan& p, const void* q, const void* k, const void* v,
+                           const int32_t* q_offsets, const int32_t* kv_offsets, const int32_t* q_lens, const int32_t* kv_lens,
+                           float softmax_scale, int f16, float* scale_out)
+{
+    if (!(softmax_scale >= 0.0f) || !isfinite(softmax_scale)) return F3D_ERR_INVALID_ARG;
+    if ((!q_offsets || !kv_offsets) && s.n_segments != 1) return F3D_ERR_INVALID_ARG;
+    if ((s.n_q > 0 && !q) || (s.n_kv > 0 && (!k || !v))) return F3D_ERR_INVALID_ARG;
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v) & 15) return F3D_ERR_BAD_ALIGNMENT;
+    if (((uintptr_t)q_offsets | (uintptr_t)kv_offsets | (uintptr_t)q_lens | (uintptr_t)kv_lens) & 3) return F3D_ERR_BAD_ALIGNMENT;
+    if ((long long)p.slots * s.kv_heads * p.parts > 2000000000ll || (long long)p.kv_slots * s.kv_heads * p.row_parts > 2000000000ll)
+        return F3D_ERR_UNSUPPORTED;
+    memset(&a, 0, sizeof(a));
+    a.q = (const uint16_t*)q;
+    a.k = (const uint16_t*)k;
+    a.v = (const uint16_t*)v;
+    a.q_offsets = q_offsets;
+    a.kv_offsets = kv_offsets;
+    a.q_lens = q_lens;
+    a.kv_lens = kv_lens;
+    a.n_q = (int)s.n_q;
+    a.n_kv = (int)s.n_kv;
+    a.segments = s.n_segments;
+    a.H = s.heads;
+    a.K = s.kv_heads;
+    a.G = s.heads / s.kv_heads;
+    a.by_g = f3d::make_divide(a.G, s.n_q * a.G);
+    const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / sqrtf((float)s.head_dim);
+    const float c_log2 = scale * 1.44269504088896340736f;
+    a.q_pow2 = 1.0f;
+    a.s_mul = c_log2;
+    if (f16) {
+        a.s_mul = fminf(c_log2, 0x1p90f);   // as in f3d_bucket_swin_attn_f16
+    } else if (c_log2 < 1.0f) {             // c_log2 = q_pow2 * s_mul, 1 <= s_mul < 2
+        int e = 0;
+        a.s_mul = 2.0f * frexpf(c_log2, &e);
+        a.q_pow2 = ldexpf(1.0f, e - 1);
+    }
+    a.f16 = f16;
+    a.few = p.few;
+    a.row_tiles = p.row_tiles;
+    a.slots = p.slots;
+    a.parts = p.parts;
+    a.chunk = p.chunk;
+    *scale_out = scale;
+    return F3D_OK;
+}
+
+int f3d_cross_attn_workspace_bytes(int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q, int64_t max_kv, int32_t heads,
+                                   int32_t kv_heads, int32_t head_dim, size_t* out_bytes)
+{
+    if (!out_bytes) return F3D_ERR_INVALID_ARG;
+    CrossSizes s;
+    const int rc = cross_sizes(s, n_q, n_kv, n_segments, max_q, max_kv, heads, kv_heads, head_dim);
+    if (rc != F3D_OK) return rc;
+    const f3d::CrossPlan p = cross_plan(s, false);
+    *out_bytes = cross_part_bytes(s, p) + cross_ml_bytes(s, p);
+    return F3D_OK;
+}
+
+static int cross_forward(int f16, const void* q, const void* k, const void* v, const int32_t* q_offsets, const int32_t* kv_offsets,
+                         const int32_t* q_lens, const int32_t* kv_lens, int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q,
+                         int64_t max_kv, int32_t heads, int32_t kv_heads, int32_t head_dim, float softmax_scale, void* out, float* lse,
+                         void* workspace, size_t workspace_bytes, void* stream)
+{
+    CrossSizes s;
+    int rc = cross_sizes(s, n_q, n_kv, n_segments, max_q, max_kv, heads, kv_heads, head_dim);
+    if (rc != F3D_OK) return rc;
+    const f3d::CrossPlan p = cross_plan(s, false);
+    f3d::CrossArgs a;
+    float scale;
+    rc = fill_cross_args(a, s, p, q, k, v, q_offsets, kv_offsets, q_lens, kv_lens, softmax_scale, f16, &scale);
+    if (rc != F3D_OK) return rc;
+    if (n_q == 0) return F3D_OK;
+    if (!out) return F3D_ERR_INVALID_ARG;
+    if ((uintptr_t)out & 15 || (uintptr_t)lse & 3) return F3D_ERR_BAD_ALIGNMENT;
+    const size_t part = cross_part_bytes(s, p), need = part + cross_ml_bytes(s, p);
+    if (need > 0) {
+        if (!workspace) return F3D_ERR_INVALID_ARG;
+        if ((uintptr_t)workspace & 255) return F3D_ERR_BAD_ALIGNMENT;
+        if (workspace_bytes < need) return F3D_ERR_WORKSPACE_TOO_SMALL;
+        a.part_o = (float*)workspace;
+        a.part_ml = (float2*)((char*)workspace + part);
+    }
+    a.out = (uint16_t*)out;
+    a.lse = lse;
+    (void)hipGetLastError();
+    const hipError_t e = f3d::cross_launch(a, head_dim, (hipStream_t)stream);
+    return e == hipSuccess ? F3D_OK : hip_fail(e);
+}
+
+int f3d_cross_attn(const void* q, const void* k, const void* v, const int32_t* q_offsets, const int32_t* kv_offsets, const int32_t* q_lens,
+                   const int32_t* kv_lens, int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q, int64_t max_kv, int32_t heads,
+                   int32_t kv_heads, int32_t head_dim, float softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                   void* stream)
+{
+    return cross_forward(0, q, k, v, q_offsets, kv_offsets, q_lens, kv_lens, n_q, n_kv, n_segments, max_q, max_kv, heads, kv_heads,
+                         head_dim, softmax_scale, out, lse, workspace, workspace_bytes, stream);
+}
+
+int f3d_cross_attn_f16(const void* q, const void* k, const void* v, const int32_t* q_offsets, const int32_t* kv_offsets, const int32_t* q_lens,
+                       const int32_t* kv_lens, int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q, int64_t max_kv, int32_t heads,
+                       int32_t kv_heads, int32_t head_dim, float softmax_scale, void* out, float* lse, void* workspace,
+                       size_t workspace_bytes, void* stream)
+{
+    return cross_forward(1, q, k, v, q_offsets, kv_offsets, q_lens, kv_lens, n_q, n_kv, n_segments, max_q, max_kv, heads, kv_heads,
+                         head_dim, softmax_scale, out, lse, workspace, workspace_bytes, stream);
+}
+
+static size_t cross_dsum_bytes(const CrossSizes& s) { return align_up((size_t)s.n_q * s.heads * sizeof(float), 256); }
+
+static size_t cross_dkv_bytes(const CrossSizes& s, const f3d::CrossPlan& p)
+{
+    return p.row_parts > 1 ? align_up((size_t)2 * p.row_parts * s.n_kv * s.kv_heads * s.head_dim * sizeof(float), 256) : 0;
+}
+
+int f3d_cross_attn_bwd_workspace_bytes(int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q, int64_t max_kv, int32_t heads,
+                                       int32_t kv_heads, int32_t head_dim, size_t* out_bytes)
+{
+    if (!out_bytes) return F3D_ERR_INVALID_ARG;
+    CrossSizes s;
+    const int rc = cross_sizes(s, n_q, n_kv, n_segments, max_q, max_kv, heads, kv_heads, head_dim);
+    if (rc != F3D_OK) return rc;
+    const f3d::CrossPlan p = cross_plan(s, true);
+    *out_bytes = cross_dsum_bytes(s) + cross_part_bytes(s, p) + cross_dkv_bytes(s, p);
+    return F3D_OK;
+}
+
+int f3d_cross_attn_bwd(const void* q, const void* k, const void* v, const void* out, const void* dout, const float* lse,
+                       const int32_t* q_offsets, const int32_t* kv_offsets, const int32_t* q_lens, const int32_t* kv_lens, int64_t n_q,
+                       int64_t n_kv, int32_t n_segments, int64_t max_q, int64_t max_kv, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                       float softmax_scale, void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream)
+{
+    CrossSizes s;
+    int rc = cross_sizes(s, n_q, n_kv, n_segments, max_q, max_kv, heads, kv_heads, head_dim);
+    if (rc != F3D_OK) return rc;
+    const f3d::CrossPlan p = cross_plan(s, true);
+    f3d::CrossBwdArgs b;
+    memset(&b, 0, sizeof(b));
+    rc = fill_cross_args(b.f, s, p, q, k, v, q_offsets, kv_offsets, q_lens, kv_lens, softmax_scale, 0, &b.scale);
+    if (rc != F3D_OK) return rc;
+    if (n_q == 0 && n_kv == 0) return F3D_OK;
+    if ((n_q > 0 && (!out || !dout || !lse || !dq)) || (n_kv > 0 && (!dk || !dv))) return F3D_ERR_INVALID_ARG;
+    if (((uintptr_t)out | (uintptr_t)dout | (uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv) & 15 || (uintptr_t)lse & 3) return F3D_ERR_BAD_ALIGNMENT;
+    const size_t dsum = cross_dsum_bytes(s), part = cross_part_bytes(s, p), need = dsum + part + cross_dkv_bytes(s, p);
+    if (need > 0) {
+        if (!workspace) return F3D_ERR_INVALID_ARG;
+        if ((uintptr_t)workspace & 255) return F3D_ERR_BAD_ALIGNMENT;
+        if (workspace_bytes < need) return F3D_ERR_WORKSPACE_TOO_SMALL;
+    }
+    b.f.out = (uint16_t*)const_cast<void*>(out);
+    b.f.lse = const_cast<float*>(lse);
+    b.dout = (const uint16_t*)dout;
+    b.dsum = (float*)workspace;
+    b.dq = (uint16_t*)dq;
+    b.dk = (uint16_t*)dk;
+    b.dv = (uint16_t*)dv;
+    b.part_dq = (float*)((char*)workspace + dsum);
+    b.part_dkv = (float*)((char*)workspace + dsum + part);
+    b.kv_slots = p.kv_slots;
+    b.row_parts = p.row_parts;
+    b.row_chunk = p.row_chunk;
+    (void)hipGetLastError();
+    const hipError_t e = f3d::cross_bwd_launch(b, head_dim, (hipStream_t)stream);
     return e == hipSuccess ? F3D_OK : hip_fail(e);
 }
 

@@ -80,3 +80,55 @@ def test_clip_grads_refuses_outputs_that_share_memory():
     assert clip([(a, 100, 2), (b, 100, 2)], [b, a]) == INVALID                 # another's gradient
     assert clip([(a, 100, 2)], [a + 4]) == INVALID                             # its own gradient, moved
     assert clip([(a, 2000, 2), (a + 400, 10, 2)], [b + 8192, a + 4000]) == INVALID   # inside a long one that began earlier
+
+
+def cross(entry="f3d_cross_attn", **kw):
+    a = dict(q=AT, k=AT, v=AT, q_offsets=AT, kv_offsets=AT, q_lens=None, kv_lens=None, n_q=100, n_kv=50, n_segments=3, max_q=60, max_kv=40,
+             heads=8, kv_heads=2, head_dim=32, scale=0.0, out=AT, lse=AT, workspace=AT, workspace_bytes=1 << 40, stream=None)
+    a.update(kw)
+    return getattr(f3d.lib(), entry)(*a.values())
+
+
+def cross_bwd(**kw):
+    a = dict(q=AT, k=AT, v=AT, out=AT, dout=AT, lse=AT, q_offsets=AT, kv_offsets=AT, q_lens=None, kv_lens=None, n_q=100, n_kv=50, n_segments=3,
+             max_q=60, max_kv=40, heads=8, kv_heads=2, head_dim=32, scale=0.0, dq=AT, dk=AT, dv=AT, workspace=AT, workspace_bytes=1 << 40,
+             stream=None)
+    a.update(kw)
+    return f3d.lib().f3d_cross_attn_bwd(*a.values())
+
+
+SHARED = [
+    (dict(n_q=-1), INVALID), (dict(n_kv=-1), INVALID), (dict(n_segments=0), INVALID), (dict(max_q=-1), INVALID), (dict(max_kv=-2), INVALID),
+    (dict(heads=0), INVALID), (dict(kv_heads=0), INVALID), (dict(heads=8, kv_heads=3), INVALID), (dict(head_dim=24), UNSUPPORTED),
+    (dict(head_dim=256), UNSUPPORTED), (dict(n_segments=65536), UNSUPPORTED), (dict(n_q=1 << 29), UNSUPPORTED), (dict(n_kv=1 << 31), UNSUPPORTED),
+    (dict(heads=4096, kv_heads=4096), UNSUPPORTED), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
+    (dict(scale=float("inf")), INVALID), (dict(q=None), INVALID), (dict(k=None), INVALID), (dict(v=None), INVALID),
+    (dict(q_offsets=None), INVALID), (dict(kv_offsets=None), INVALID), (dict(q=AT + 8), ALIGN), (dict(v=AT + 2), ALIGN),
+    (dict(kv_lens=AT + 1), ALIGN), (dict(q_offsets=AT + 2), ALIGN), (dict(out=None), INVALID), (dict(out=AT + 8), ALIGN), (dict(lse=AT + 2), ALIGN)]
+LONG = dict(n_q=3, n_kv=30000, max_q=1, max_kv=10000)       # the keys are split: a workspace is needed
+
+
+@pytest.mark.parametrize("kw,code", SHARED + [
+    ({**LONG, "workspace": None}, INVALID), ({**LONG, "workspace": AT + 16}, ALIGN), ({**LONG, "workspace_bytes": 100}, SMALL),
+    (dict(n_q=0, q=None, out=None), OK)])
+def test_cross_attn_refuses(kw, code):
+    assert cross(**kw) == code
+    assert cross("f3d_cross_attn_f16", **kw) == code
+
+
+@pytest.mark.parametrize("kw,code", SHARED + [
+    (dict(workspace=None), INVALID), (dict(workspace=AT + 128), ALIGN), (dict(workspace_bytes=100 * 8 * 4 - 1), SMALL), (dict(dout=None), INVALID),
+    (dict(lse=None), INVALID), (dict(dq=None), INVALID), (dict(dk=None), INVALID), (dict(dv=None), INVALID), (dict(dk=AT + 4), ALIGN),
+    (dict(n_q=0, n_kv=0, q=None, k=None, v=None, out=None, workspace=None), OK)])
+def test_cross_attn_bwd_refuses(kw, code):
+    assert cross_bwd(**kw) == code
+
+
+def test_cross_attn_workspace_refuses():
+    size = ctypes.c_size_t(0)
+    for name in ("f3d_cross_attn_workspace_bytes", "f3d_cross_attn_bwd_workspace_bytes"):
+        call = getattr(f3d.lib(), name)
+        assert call(10, 10, 1, 0, 0, 4, 2, 32, None) == INVALID
+        assert call(10, 10, 1, 0, 0, 4, 3, 32, ctypes.byref(size)) == INVALID
+        assert call(10, 10, 1, 0, 0, 4, 2, 40, ctypes.byref(size)) == UNSUPPORTED
+        assert call(10, 10, 1, 0, 0, 4, 2, 32, ctypes.byref(size)) == OK
