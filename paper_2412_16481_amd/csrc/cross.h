@@ -26,12 +26,18 @@ struct CrossArgs {
     int f16;
     int few;                    // the form for few query rows
     int row_tiles;              // tiles of 32 query rows a wave owns
-    int slots;                  // row blocks over all segments (upper bound, surplus workgroups exit)
+    int run_shift;              // a workgroup takes 2^run_shift rows of a segment
+    int slots;                  // such runs over all segments (upper bound, surplus workgroups exit)
+    int turn;                   // consecutive pieces of work that go to one XCD
     int parts;                  // parts the keys of a segment are split into
     int chunk;                  // keys of a part
     float* part_o;              // [parts][n_q * H][head_dim], sums of a part relative to its largest score
     float2* part_ml;            // [parts][n_q * H]: that score (log2 units), sum of exponentials
 };
+
+// consecutive pieces (row blocks x parts x key/value heads) to an XCD: the heads of up to eight blocks; the grid is whole rounds of eight turns
+inline int cross_turn(long long blocks, int kv_heads) { return kv_heads * (int)(blocks < 64 ? 1 : blocks < 512 ? blocks / 64 : 8); }
+inline unsigned cross_grid(long long blocks, int kv_heads, int turn) { return (unsigned)((blocks * kv_heads + 8ll * turn - 1) / (8ll * turn) * 8 * turn); }
 
 struct CrossBwdArgs {
     CrossArgs f;                // parts and chunk of the query gradient's kernel
@@ -42,6 +48,7 @@ struct CrossBwdArgs {
     uint16_t* dv;
     float scale;
     float* part_dq;             // [parts][n_q * H][head_dim], where parts > 1
+    int kv_turn;
     int kv_slots;               // blocks of 128 keys over all segments
     int row_parts;              // parts the query rows of a segment are split into
     int row_chunk;              // rows of a part
@@ -50,7 +57,7 @@ struct CrossBwdArgs {
 
 // What a call takes: a rule on sizes the host knows
 struct CrossPlan {
-    int few, row_tiles, slots, parts, chunk;
+    int few, row_tiles, run_shift, slots, parts, chunk;
     int kv_slots, row_parts, row_chunk;   // backward
 };
 CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_q, long long max_kv, int heads, int kv_heads, int head_dim, bool backward);

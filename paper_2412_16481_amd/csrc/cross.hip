@@ -26,47 +26,310 @@ namespace {
 
 constexpr float LN2 = 0.6931471805599453f;
 
-template <int D, bool FEW>
-struct Stage {
+// Keys stream through LDS in stages, three of them resident; a wave owns QT tiles of 32 rows at a time.
+template <int D>
+struct RowStage {
     using T = Tile<D>;
-    static constexpr int ROWS = !FEW && D == 128 ? 64 : 128;   // keys
+    static constexpr int WAVES = D == 128 ? 8 : 4;    // 128: three stages leave room for one workgroup on a compute unit
+    static constexpr int ROWS = D <= 32 ? 128 : 64;
     static constexpr int TILES = ROWS / 32;
-    static constexpr int BYTES = ROWS * T::ROWB;               // of K, and of V
-    static constexpr int NBUF = D >= 64 ? 2 : 3;
-    static constexpr int LPW = ROWS * T::NC / 256;             // loads per lane, stage and tensor
+    static constexpr int BYTES = ROWS * T::ROWB;      // of K, and of V
+    static constexpr int NBUF = 3;
+    static constexpr int LPW = ROWS * T::NC / (64 * WAVES);
     static constexpr int TOTAL = NBUF * 2 * BYTES;
 };
 
-template <int D, int QT, bool FEW, bool F16, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a)
+template <int D, int QT, bool F16, bool SPLIT>
+__global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs a)
 {
     using T = Tile<D>;
-    using S = Stage<D, FEW>;
+    using S = RowStage<D>;
+    using E = Half<F16>;
+    constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF, NW = S::WAVES;
+    constexpr int BM = 32 * QT * NW;                  // rows of a workgroup at a time
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[S::TOTAL];
+    const uint32_t sK = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sV = sK + NBUF * S::BYTES;
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    // which (run of row blocks, part, key/value head): consecutive ids stay on one XCD, the heads of the same rows beside each other
+    const uint32_t u = piece_of(a.turn);
+    const uint32_t x = u / (uint32_t)a.K;
+    const int kh = (int)(u - x * a.K), slot = (int)(SPLIT ? x / (uint32_t)a.parts : x), part = SPLIT ? (int)(x - (uint32_t)slot * a.parts) : 0;
+    if (slot >= a.slots) return;
+    const int b = segment_of(a.q_offsets, a.n_q, a.segments, a.G, a.run_shift, slot);
+    const Rows qs = rows_of(a.q_offsets, a.q_lens, a.n_q, b), kv = rows_of(a.kv_offsets, a.kv_lens, a.n_kv, b);
+    const long long run = slot - first_slot(a.q_offsets, a.n_q, b, a.G, a.run_shift);
+    const long long rows = (long long)qs.span * a.G, live = (long long)qs.len * a.G, first_row = run << a.run_shift;
+    if (run < 0 || first_row >= rows) return;
+    const int blocks = (int)((min(rows, first_row + (1ll << a.run_shift)) - first_row + BM - 1) / BM);
+    const int key0 = SPLIT ? part * a.chunk : 0;
+    const int nkeys = first_row >= live ? 0 : SPLIT ? min(max(kv.len - key0, 0), a.chunk) : kv.len;   // this workgroup's
+
+    // ---- staging
+    const uint32_t row_bytes = (uint32_t)a.K * T::ROWB;
+    const uint64_t first = (uint64_t)(kv.from + key0) * row_bytes + (uint64_t)kh * T::ROWB;
+    int srow[LPW];
+    uint32_t scol[LPW];
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+        const int p = (wave * LPW + i) * 64 + lane;
+        srow[i] = p / T::NC;
+        scol[i] = ((p % T::NC) ^ T::swizzle(srow[i])) << 4;
+    }
+    auto request = [&](int st, int buf) __attribute__((always_inline)) {
+        const uint32_t to = buf * S::BYTES;
+#pragma unroll
+        for (int i = 0; i < LPW; ++i) {
+            const int key = min(st * S::ROWS + srow[i], nkeys - 1);   // past the end: the last key again, masked
+            const uint64_t at = first + (uint64_t)(uint32_t)key * row_bytes + scol[i];
+            lds_dma16(reinterpret_cast<const char*>(a.k) + at, sK + to + (wave * LPW + i) * 1024);
+            lds_dma16(reinterpret_cast<const char*>(a.v) + at, sV + to + (wave * LPW + i) * 1024);
+        }
+    };
+    const int nst = (nkeys + S::ROWS - 1) / S::ROWS;
+    const bool stays = nst <= NBUF;                   // all keys are resident: staged once, and no barrier behind the first
+    const int total = stays ? nst : nst * blocks;     // stages to come, over all row blocks
+    int asked = 0, ask_st = 0;                        // stages requested, the next one's keys
+    auto request_next = [&](int buf) __attribute__((always_inline)) {
+        request(ask_st, buf);
+        ++asked;
+        ask_st = ask_st + 1 == nst ? 0 : ask_st + 1;
+    };
+    if (total > 0) request_next(0);
+    if (total > 1) request_next(1);
+    if (stays && total > 2) request_next(2);
+
+    uint32_t koff[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) koff[ks] = sK + T::row_piece(lane, ks);
+    const uint32_t voff = sV + T::transposed(lane);
+    const float mul = a.s_mul;
+
+    // this lane's rows: row l32 of each of the wave's tiles
+    U4 qf[QT][KS];
+    auto row_of = [&](int blk, int t) __attribute__((always_inline)) { return first_row + (long long)blk * BM + wave * 32 * QT + t * 32 + l32; };
+    auto place_of = [&](long long row) __attribute__((always_inline)) {   // (query, head) of the tensor; past the end: of the last row
+        const int r = (int)min(row, rows - 1), i = divide(r, a.G, a.by_g), g = r - i * a.G;
+        return (size_t)(qs.from + i) * a.H + kh * a.G + g;
+    };
+    auto fetch_rows = [&](int blk) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const uint16_t* const from = a.q + place_of(row_of(blk, t)) * D + hf * 8;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) qf[t][ks].u = *reinterpret_cast<const uint4*>(from + ks * 16);
+        }
+    };
+    fetch_rows(0);
+    if (total > 0) {
+        __builtin_amdgcn_s_waitcnt(vm_wait(0));
+        __syncthreads();                              // the stages asked for so far are here
+    }
+
+    f32x16 o[QT][MT], sa, sb;
+    float m[QT], l[QT];                               // reference of the exponentials (log2 units), their sum over this lane's keys
+    U4 kf[KS];
+    auto read_k = [&](U4 (&f)[KS], uint32_t at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) f[ks].u = lds_read16(koff[ks] + at);
+    };
+    // One unit of the pipeline: the softmax of the score tile `s` (row tile t, keys from kbase on) and O^T += V^T P^T from the keys at
+    // `at`, with the MFMAs of the NEXT score tile (`sn`, rows of tile tn, keys in kf) in between.
+    auto unit = [&](f32x16& s, int t, uint32_t at, int kbase, f32x16& sn, int tn) __attribute__((always_inline)) {
+        U4 p0, p1, v0[2], v1[2];
+        if (kbase + 32 > nkeys) {                     // the last tile may be short
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (kbase + 8 * (r >> 2) + 4 * hf + (r & 3) >= nkeys) s[r] = -INFINITY;
+        }
+        float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
+#pragma unroll
+        for (int r = 3; r < 15; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
+        mx = fmaxf(mx, s[15]);
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);   // the row's other keys
+        mx = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1])) * mul;
+        if (__builtin_amdgcn_ballot_w64(mx > m[t] + 8.0f)) {
+            const float top = fmaxf(m[t], mx), alpha = __builtin_amdgcn_exp2f(m[t] - top);   // the first time 2^-inf, onto zeros
+            m[t] = top;
+            l[t] *= alpha;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[t][mt][r] *= alpha;
+            }
+        }
+        const auto prob = [&](int r) __attribute__((always_inline)) { s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], mul, -m[t])); };
+        constexpr int EP = 16 / KS;
+        F3D_SB();
+        read_transposed<D>(v0[0], v1[0], voff + at, (voff + at) ^ T::FLIP, 0);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+            for (int e = 0; e < EP; ++e) prob(ks * EP + e);
+            F3D_SB();
+            sn = E::mfma(kf[ks], qf[tn][ks], ks == 0 ? f32x16{0} : sn);
+            F3D_SB();
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) (&p0.u.x)[e] = E::pack(s[2 * e], s[2 * e + 1]);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            if (mt + 1 < MT) read_transposed<D>(v0[(mt + 1) & 1], v1[(mt + 1) & 1], voff + at, (voff + at) ^ T::FLIP, mt + 1);
+            F3D_SB();
+            o[t][mt] = E::mfma(v0[mt & 1], p0, o[t][mt]);
+            F3D_SB();
+            if (mt == 0) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) (&p1.u.x)[e] = E::pack(s[8 + 2 * e], s[8 + 2 * e + 1]);
+            }
+            F3D_SB();
+            o[t][mt] = E::mfma(v1[mt & 1], p1, o[t][mt]);
+            F3D_SB();
+#pragma unroll
+            for (int r = mt * (16 / MT); r < (mt + 1) * (16 / MT); ++r) l[t] += s[r];
+        }
+    };
+
+    int buf = 0;
+    for (int blk = 0; blk < blocks; ++blk) {
+        const bool busy = first_row + (long long)blk * BM + wave * 32 * QT < live;   // this wave has rows with results
+        if (!F16) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) qf[t][ks] = scale_pow2(qf[t][ks], a.q_pow2);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            m[t] = -INFINITY;
+            l[t] = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) o[t][mt] = f32x16{0};
+        }
+        if (stays) buf = 0;
+        if (nst > 0) {
+            read_k(kf, buf * S::BYTES);
+            sa = f32x16{0};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) sa = E::mfma(kf[ks], qf[0][ks], sa);
+        }
+        for (int st = 0; st < nst; ++st) {
+            const int bufn = buf + 1 == NBUF ? 0 : buf + 1;
+            const uint32_t at0 = buf * S::BYTES, an0 = bufn * S::BYTES;
+#pragma unroll
+            for (int t4 = 0; t4 < S::TILES; ++t4) {
+                if (t4 + 1 == S::TILES && !stays) {
+                    // The next stage is handed over to the readers, and the buffer of the one before this is asked for again: whoever
+                    // arrives has its own loads of the next stage and has read the last of the one before.
+                    __builtin_amdgcn_s_waitcnt(vm_wait(0));
+                    __syncthreads();
+                    if (asked < total) request_next(bufn + 1 == NBUF ? 0 : bufn + 1);
+                }
+                const int kbase = st * S::ROWS + t4 * 32;
+                if (!busy || kbase >= nkeys) continue;
+                const uint32_t at = at0 + t4 * T::BYTES, an = t4 + 1 < S::TILES ? at + T::BYTES : an0;
+                if (QT == 1) {
+                    read_k(kf, an);                   // what is computed ahead of the last tile is never used
+                    if ((t4 & 1) == 0) unit(sa, 0, at, kbase, sb, 0);
+                    else unit(sb, 0, at, kbase, sa, 0);
+                } else {
+                    unit(sa, 0, at, kbase, sb, QT - 1);
+                    read_k(kf, an);
+                    unit(sb, QT - 1, at, kbase, sa, 0);
+                }
+            }
+            buf = bufn;
+        }
+        // ---- results; the next block's rows are on their way meanwhile
+        size_t at_q[QT];
+        bool mine[QT], has[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const long long row = row_of(blk, t);
+            mine[t] = row < rows;
+            has[t] = row < live && nkeys > 0;
+            at_q[t] = place_of(row);
+        }
+        if (blk + 1 < blocks) fetch_rows(blk + 1);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(l[t]), __float_as_int(l[t]), false, false);
+            l[t] = __int_as_float(sw[0]) + __int_as_float(sw[1]);
+            if (!mine[t]) continue;
+            if (SPLIT) {
+                const size_t pa = (size_t)part * a.n_q * a.H + at_q[t];
+                if (hf == 0) a.part_ml[pa] = has[t] ? make_float2(m[t], l[t]) : make_float2(-INFINITY, 0.f);
+                if (!has[t]) continue;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                    for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4)
+                        *reinterpret_cast<float4*>(a.part_o + pa * D + mt * 32 + 8 * r4 + 4 * hf) =
+                            make_float4(o[t][mt][4 * r4], o[t][mt][4 * r4 + 1], o[t][mt][4 * r4 + 2], o[t][mt][4 * r4 + 3]);
+                }
+                continue;
+            }
+            const float inv = 1.0f / l[t];
+            if (a.lse && hf == 0) a.lse[at_q[t]] = has[t] ? (m[t] + __log2f(l[t])) * LN2 : -INFINITY;
+            uint16_t* const to = a.out + at_q[t] * D;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4) {
+                    uint2 y = make_uint2(0, 0);
+                    if (has[t]) {
+                        y.x = E::pack(o[t][mt][4 * r4] * inv, o[t][mt][4 * r4 + 1] * inv);
+                        y.y = E::pack(o[t][mt][4 * r4 + 2] * inv, o[t][mt][4 * r4 + 3] * inv);
+                    }
+                    *reinterpret_cast<uint2*>(to + mt * 32 + 8 * r4 + 4 * hf) = y;
+                }
+            }
+        }
+    }
+}
+
+// Few query rows: the keys of a stage, 128 of them, are shared out to the waves
+template <int D>
+struct FewStage {
+    using T = Tile<D>;
+    static constexpr int ROWS = 128;
+    static constexpr int BYTES = ROWS * T::ROWB;      // of K, and of V
+    static constexpr int NBUF = D >= 64 ? 2 : 3;
+    static constexpr int LPW = ROWS * T::NC / 256;    // loads per lane, stage and tensor
+    static constexpr int TOTAL = NBUF * 2 * BYTES;
+};
+
+template <int D, bool F16, bool SPLIT>
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a)
+{
+    using T = Tile<D>;
+    using S = FewStage<D>;
     using E = Half<F16>;
     constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF;
-    constexpr int BM = FEW ? 32 : 128 * QT, SHIFT = FEW ? 5 : QT == 2 ? 8 : 7;   // rows of a workgroup
-    static_assert(!FEW || QT == 1, "one tile of rows");
+    constexpr int BM = 32, SHIFT = 5;                 // rows of a workgroup
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::TOTAL];
     const uint32_t sK = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sV = sK + NBUF * S::BYTES;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
     // which (row block, part, key/value head): consecutive ids stay on one XCD, the heads of the same rows beside each other
-    const uint32_t u = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    const uint32_t u = piece_of(a.turn);
     const uint32_t x = u / (uint32_t)a.K;
     const int kh = (int)(u - x * a.K), slot = (int)(SPLIT ? x / (uint32_t)a.parts : x), part = SPLIT ? (int)(x - (uint32_t)slot * a.parts) : 0;
     if (slot >= a.slots) return;
     const int b = segment_of(a.q_offsets, a.n_q, a.segments, a.G, SHIFT, slot);
-    const Rows qs = rows_of(a.q_offsets, a.q_lens, a.n_q, b), ks_ = rows_of(a.kv_offsets, a.kv_lens, a.n_kv, b);
+    const Rows qs = rows_of(a.q_offsets, a.q_lens, a.n_q, b), kv = rows_of(a.kv_offsets, a.kv_lens, a.n_kv, b);
     const long long blk = slot - first_slot(a.q_offsets, a.n_q, b, a.G, SHIFT);
     const long long rows = (long long)qs.span * a.G, live = (long long)qs.len * a.G;
     if (blk < 0 || blk * BM >= rows) return;
     const int key0 = SPLIT ? part * a.chunk : 0;
-    const int nkeys = blk * BM >= live ? 0 : SPLIT ? min(max(ks_.len - key0, 0), a.chunk) : ks_.len;   // this workgroup's
+    const int nkeys = blk * BM >= live ? 0 : SPLIT ? min(max(kv.len - key0, 0), a.chunk) : kv.len;   // this workgroup's
 
     // ---- staging
     const uint32_t row_bytes = (uint32_t)a.K * T::ROWB;
-    const uint64_t first = (uint64_t)(ks_.from + key0) * row_bytes + (uint64_t)kh * T::ROWB;
+    const uint64_t first = (uint64_t)(kv.from + key0) * row_bytes + (uint64_t)kh * T::ROWB;
     int srow[LPW];
     uint32_t scol[LPW];
 #pragma unroll
@@ -89,29 +352,15 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a)
     if (nst > 0) dma_stage(0);
     if (NBUF > 2 && nst > 1) dma_stage(1);
 
-    // ---- this lane's rows: row l32 of each of the wave's tiles
-    U4 qf[QT][KS];
-    long long row[QT];                                // row of the segment, -1: none
-    size_t at_q[QT];                                  // (query, head) of the tensor
-    bool takes[QT];
+    // ---- this lane's row: row l32
+    U4 qf[KS];
+    {
+        const int r = (int)min(blk * BM + l32, rows - 1), i = divide(r, a.G, a.by_g), g = r - i * a.G;   // past the end: the last row again
+        const uint16_t* const from = a.q + ((size_t)(qs.from + i) * a.H + kh * a.G + g) * D + hf * 8;
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        row[t] = blk * BM + (FEW ? 0 : wave * 32 * QT) + t * 32 + l32;
-        const int r = (int)min(row[t], rows - 1);     // past the end: the last row again, never stored
-        const int i = divide(r, a.G, a.by_g), g = r - i * a.G;
-        takes[t] = row[t] < live;
-        if (row[t] >= rows) row[t] = -1;
-        at_q[t] = (size_t)(qs.from + i) * a.H + kh * a.G + g;
-        const uint16_t* const from = a.q + at_q[t] * D + hf * 8;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) qf[t][ks].u = *reinterpret_cast<const uint4*>(from + ks * 16);
-    }
-    const bool busy = FEW || blk * BM + wave * 32 * QT < live;   // this wave has rows with results
-    if (!F16) {
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) qf[t][ks] = scale_pow2(qf[t][ks], a.q_pow2);
+        for (int ks = 0; ks < KS; ++ks) {
+            qf[ks].u = *reinterpret_cast<const uint4*>(from + ks * 16);
+            if (!F16) qf[ks] = scale_pow2(qf[ks], a.q_pow2);
         }
     }
     uint32_t koff[KS];
@@ -120,74 +369,55 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a)
     const uint32_t voff = sV + T::transposed(lane);
     const float mul = a.s_mul;
 
-    f32x16 o[QT][MT];
-    float m[QT], l[QT];                               // reference of the exponentials (log2 units), their sum over this lane's keys
+    f32x16 o[MT];
+    float m = -INFINITY, l = 0.f;                     // reference of the exponentials (log2 units), their sum over this lane's keys
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        m[t] = -INFINITY;
-        l[t] = 0.f;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) o[t][mt] = f32x16{0};
-    }
+    for (int mt = 0; mt < MT; ++mt) o[mt] = f32x16{0};
 
     auto tile = [&](uint32_t at, int kbase) __attribute__((always_inline)) {
-        U4 kf[KS];
-        f32x16 s[QT];
-        U4 p0[QT], p1[QT];
+        U4 kf[KS], p0, p1;
+        f32x16 s = f32x16{0};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) kf[ks].u = lds_read16(koff[ks] + at);
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            s[t] = f32x16{0};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s[t] = E::mfma(kf[ks], qf[t][ks], s[t]);
-        }
+        for (int ks = 0; ks < KS; ++ks) s = E::mfma(kf[ks], qf[ks], s);
         if (kbase + 32 > nkeys) {                     // the last tile may be short
 #pragma unroll
-            for (int t = 0; t < QT; ++t) {
+            for (int r = 0; r < 16; ++r)
+                if (kbase + 8 * (r >> 2) + 4 * hf + (r & 3) >= nkeys) s[r] = -INFINITY;
+        }
+        float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (kbase + 8 * (r >> 2) + 4 * hf + (r & 3) >= nkeys) s[t][r] = -INFINITY;
+        for (int r = 3; r < 15; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
+        mx = fmaxf(mx, s[15]);
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);   // the row's other keys
+        mx = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1])) * mul;
+        if (__builtin_amdgcn_ballot_w64(mx > m + 8.0f)) {
+            const float top = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - top);   // the first time 2^-inf, onto zeros
+            m = top;
+            l *= alpha;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[mt][r] *= alpha;
             }
         }
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            float mx = fmaxf(fmaxf(s[t][0], s[t][1]), s[t][2]);
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], mul, -m));
+            l += s[r];
+        }
 #pragma unroll
-            for (int r = 3; r < 15; r += 2) mx = fmaxf(fmaxf(mx, s[t][r]), s[t][r + 1]);
-            mx = fmaxf(mx, s[t][15]);
-            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);   // the row's other keys
-            mx = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1])) * mul;
-            if (__builtin_amdgcn_ballot_w64(mx > m[t] + 8.0f)) {
-                const float top = fmaxf(m[t], mx), alpha = __builtin_amdgcn_exp2f(m[t] - top);   // the first time 2^-inf, onto zeros
-                m[t] = top;
-                l[t] *= alpha;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[t][mt][r] *= alpha;
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], mul, -m[t]));
-                l[t] += s[t][r];
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                (&p0[t].u.x)[e] = E::pack(s[t][2 * e], s[t][2 * e + 1]);
-                (&p1[t].u.x)[e] = E::pack(s[t][8 + 2 * e], s[t][8 + 2 * e + 1]);
-            }
+        for (int e = 0; e < 4; ++e) {
+            (&p0.u.x)[e] = E::pack(s[2 * e], s[2 * e + 1]);
+            (&p1.u.x)[e] = E::pack(s[8 + 2 * e], s[8 + 2 * e + 1]);
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             U4 v0, v1;
             read_transposed<D>(v0, v1, voff + at, (voff + at) ^ T::FLIP, mt);
-#pragma unroll
-            for (int t = 0; t < QT; ++t) {
-                o[t][mt] = E::mfma(v0, p0[t], o[t][mt]);
-                o[t][mt] = E::mfma(v1, p1[t], o[t][mt]);
-            }
+            o[mt] = E::mfma(v0, p0, o[mt]);
+            o[mt] = E::mfma(v1, p1, o[mt]);
         }
     };
 
@@ -197,114 +427,69 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a)
         else __builtin_amdgcn_s_waitcnt(vm_wait(0));
         __syncthreads();                              // every wave's are, and the buffer of stage st - 1 has been read
         if (st + NBUF - 1 < nst) dma_stage(st + NBUF - 1);
-        if (!busy) continue;
-        const uint32_t at = (st % NBUF) * S::BYTES;
-        if (FEW) {
-            if (st * S::ROWS + wave * 32 < nkeys) tile(at + wave * T::BYTES, st * S::ROWS + wave * 32);
-        } else {
-#pragma unroll 1
-            for (int t4 = 0; t4 < S::TILES && st * S::ROWS + t4 * 32 < nkeys; ++t4) tile(at + t4 * T::BYTES, st * S::ROWS + t4 * 32);
-        }
+        if (st * S::ROWS + wave * 32 < nkeys) tile((st % NBUF) * S::BYTES + wave * T::BYTES, st * S::ROWS + wave * 32);
     }
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(l[t]), __float_as_int(l[t]), false, false);
-        l[t] = __int_as_float(sw[0]) + __int_as_float(sw[1]);
+    {
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(l), __float_as_int(l), false, false);
+        l = __int_as_float(sw[0]) + __int_as_float(sw[1]);
     }
 
-    if constexpr (FEW) {
-        // ---- the four waves' results meet in LDS: row by row, channels in order
-        constexpr int P = D + 4;                      // floats from one row to the next
-        static_assert(4 * 32 * P * 4 <= S::TOTAL, "room for the results");
-        float* const meet = reinterpret_cast<float*>(smem);
-        __shared__ float sm_[4][32], sl_[4][32];
-        __syncthreads();                              // the last stage has been read
-        if (hf == 0) {
-            sm_[wave][l32] = m[0];
-            sl_[wave][l32] = l[0];
-        }
+    // ---- the four waves' results meet in LDS: row by row, channels in order
+    constexpr int P = D + 4;                      // floats from one row to the next
+    static_assert(4 * 32 * P * 4 <= S::TOTAL, "room for the results");
+    float* const meet = reinterpret_cast<float*>(smem);
+    __shared__ float sm_[4][32], sl_[4][32];
+    __syncthreads();                              // the last stage has been read
+    if (hf == 0) {
+        sm_[wave][l32] = m;
+        sl_[wave][l32] = l;
+    }
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+    for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-            for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4)
-                *reinterpret_cast<float4*>(meet + (wave * 32 + l32) * P + mt * 32 + 8 * r4 + 4 * hf) =
-                    make_float4(o[0][mt][4 * r4], o[0][mt][4 * r4 + 1], o[0][mt][4 * r4 + 2], o[0][mt][4 * r4 + 3]);
-        }
-        __syncthreads();
-        constexpr int EACH = D / 8;                   // channels of a thread: eight of them to a row
-        const int rr = tid >> 3, c0 = (tid & 7) * EACH;
-        const long long r = blk * BM + rr;
-        if (r >= rows) return;
-        const int i = divide((int)r, a.G, a.by_g), g = (int)r - i * a.G;
-        const size_t at = (size_t)(qs.from + i) * a.H + kh * a.G + g;
-        const bool counts = r < live;
-        const float top = fmaxf(fmaxf(sm_[0][rr], sm_[1][rr]), fmaxf(sm_[2][rr], sm_[3][rr]));
-        float w[4], sum = 0.f;
+        for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4)
+            *reinterpret_cast<float4*>(meet + (wave * 32 + l32) * P + mt * 32 + 8 * r4 + 4 * hf) =
+                make_float4(o[mt][4 * r4], o[mt][4 * r4 + 1], o[mt][4 * r4 + 2], o[mt][4 * r4 + 3]);
+    }
+    __syncthreads();
+    constexpr int EACH = D / 8;                   // channels of a thread: eight of them to a row
+    const int rr = tid >> 3, c0 = (tid & 7) * EACH;
+    const long long r = blk * BM + rr;
+    if (r >= rows) return;
+    const int i = divide((int)r, a.G, a.by_g), g = (int)r - i * a.G;
+    const size_t at = (size_t)(qs.from + i) * a.H + kh * a.G + g;
+    const bool counts = r < live;
+    const float top = fmaxf(fmaxf(sm_[0][rr], sm_[1][rr]), fmaxf(sm_[2][rr], sm_[3][rr]));
+    float w[4], sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {                 // a wave without keys has -inf, and so has `top` where all have
-            w[k] = sm_[k][rr] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm_[k][rr] - top);
-            sum += w[k] * sl_[k][rr];
-        }
-        float y[EACH];
+    for (int k = 0; k < 4; ++k) {                 // a wave without keys has -inf, and so has `top` where all have
+        w[k] = sm_[k][rr] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm_[k][rr] - top);
+        sum += w[k] * sl_[k][rr];
+    }
+    float y[EACH];
 #pragma unroll
-        for (int c = 0; c < EACH; ++c) {
-            y[c] = 0.f;
+    for (int c = 0; c < EACH; ++c) {
+        y[c] = 0.f;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (w[k] != 0.f) y[c] += w[k] * meet[(k * 32 + rr) * P + c0 + c];
-        }
-        if (!counts) sum = 0.f;
-        if (SPLIT) {
-            const size_t pa = (size_t)part * a.n_q * a.H + at;
-            if ((tid & 7) == 0) a.part_ml[pa] = make_float2(sum > 0.f ? top : -INFINITY, sum);
-            if (sum > 0.f) {
+        for (int k = 0; k < 4; ++k)
+            if (w[k] != 0.f) y[c] += w[k] * meet[(k * 32 + rr) * P + c0 + c];
+    }
+    if (!counts) sum = 0.f;
+    if (SPLIT) {
+        const size_t pa = (size_t)part * a.n_q * a.H + at;
+        if ((tid & 7) == 0) a.part_ml[pa] = make_float2(sum > 0.f ? top : -INFINITY, sum);
+        if (sum > 0.f) {
 #pragma unroll
-                for (int c = 0; c < EACH; c += 2) *reinterpret_cast<float2*>(a.part_o + pa * D + c0 + c) = make_float2(y[c], y[c + 1]);
-            }
-            return;
-        }
-        const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-        if (a.lse && (tid & 7) == 0) a.lse[at] = sum > 0.f ? (top + __log2f(sum)) * LN2 : -INFINITY;
-#pragma unroll
-        for (int c = 0; c < EACH; c += 2) {
-            const uint32_t pair = sum > 0.f ? E::pack(y[c] * inv, y[c + 1] * inv) : 0u;
-            *reinterpret_cast<uint32_t*>(a.out + at * D + c0 + c) = pair;
+            for (int c = 0; c < EACH; c += 2) *reinterpret_cast<float2*>(a.part_o + pa * D + c0 + c) = make_float2(y[c], y[c + 1]);
         }
         return;
     }
-
+    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+    if (a.lse && (tid & 7) == 0) a.lse[at] = sum > 0.f ? (top + __log2f(sum)) * LN2 : -INFINITY;
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        if (row[t] < 0) continue;
-        const bool has = takes[t] && nkeys > 0;
-        if (SPLIT) {
-            const size_t pa = (size_t)part * a.n_q * a.H + at_q[t];
-            if (hf == 0) a.part_ml[pa] = has ? make_float2(m[t], l[t]) : make_float2(-INFINITY, 0.f);
-            if (!has) continue;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-                for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4)
-                    *reinterpret_cast<float4*>(a.part_o + pa * D + mt * 32 + 8 * r4 + 4 * hf) =
-                        make_float4(o[t][mt][4 * r4], o[t][mt][4 * r4 + 1], o[t][mt][4 * r4 + 2], o[t][mt][4 * r4 + 3]);
-            }
-            continue;
-        }
-        const float inv = 1.0f / l[t];
-        if (a.lse && hf == 0) a.lse[at_q[t]] = has ? (m[t] + __log2f(l[t])) * LN2 : -INFINITY;
-        uint16_t* const to = a.out + at_q[t] * D;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-            for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4) {
-                uint2 y = make_uint2(0, 0);
-                if (has) {
-                    y.x = E::pack(o[t][mt][4 * r4] * inv, o[t][mt][4 * r4 + 1] * inv);
-                    y.y = E::pack(o[t][mt][4 * r4 + 2] * inv, o[t][mt][4 * r4 + 3] * inv);
-                }
-                *reinterpret_cast<uint2*>(to + mt * 32 + 8 * r4 + 4 * hf) = y;
-            }
-        }
+    for (int c = 0; c < EACH; c += 2) {
+        const uint32_t pair = sum > 0.f ? E::pack(y[c] * inv, y[c + 1] * inv) : 0u;
+        *reinterpret_cast<uint32_t*>(a.out + at * D + c0 + c) = pair;
     }
 }
 
@@ -343,19 +528,21 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a)
 template <int D, bool F16>
 hipError_t launch(const CrossArgs& a, hipStream_t stream)
 {
-    const long long total = ((long long)a.slots * a.K * a.parts + 7) / 8 * 8;
-    const unsigned grid = (unsigned)total;
-    constexpr int QT2 = D <= 64 ? 2 : 1;
+    const unsigned grid = cross_grid((long long)a.slots * a.parts, a.K, a.turn), threads = 64 * RowStage<D>::WAVES;
     const bool split = a.parts > 1;
     if (a.few) {
-        if (split) k_cross<D, 1, true, F16, true><<<grid, 256, 0, stream>>>(a);
-        else k_cross<D, 1, true, F16, false><<<grid, 256, 0, stream>>>(a);
+        if (split) k_cross_few<D, F16, true><<<grid, 256, 0, stream>>>(a);
+        else k_cross_few<D, F16, false><<<grid, 256, 0, stream>>>(a);
     } else if (a.row_tiles == 2) {
-        if (split) return hipErrorInvalidValue;       // two tiles a wave are for launches that fill the chip
-        k_cross<D, QT2, false, F16, false><<<grid, 256, 0, stream>>>(a);
+        if constexpr (D <= 64) {
+            if (split) return hipErrorInvalidValue;   // two tiles a wave are for launches that fill the chip
+            k_cross<D, 2, F16, false><<<grid, threads, 0, stream>>>(a);
+        } else {
+            return hipErrorInvalidValue;
+        }
     } else {
-        if (split) k_cross<D, 1, false, F16, true><<<grid, 256, 0, stream>>>(a);
-        else k_cross<D, 1, false, F16, false><<<grid, 256, 0, stream>>>(a);
+        if (split) k_cross<D, 1, F16, true><<<grid, threads, 0, stream>>>(a);
+        else k_cross<D, 1, F16, false><<<grid, threads, 0, stream>>>(a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !split) return e;
@@ -380,11 +567,12 @@ CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_
     const long long rows = n_q * group;               // of one key/value head
     p.few = max_q * group <= 32 && !backward;
     p.row_tiles = !p.few && head_dim <= (backward ? 32 : 64) && (rows / 256) * kv_heads >= 2 * CUS ? 2 : 1;
-    const int block = p.few ? 32 : 128 * p.row_tiles;
-    p.slots = (int)(rows / block + segments);
+    int block_shift = p.few ? 5 : 7 + (p.row_tiles == 2);
+    if (head_dim == 128 && !p.few && !backward) block_shift = 8;   // eight waves
     // fewer than two workgroups per compute unit: parts of 256 keys at least, until there are about three
-    const long long work = (rows + block - 1) / block < 1 ? 1 : (rows + block - 1) / block;
-    const long long blocks = (work > segments ? work : segments) * kv_heads;
+    long long work = (rows + (1ll << block_shift) - 1) >> block_shift;
+    if (work < segments) work = segments;
+    const long long blocks = work * kv_heads;
     long long parts = 1;
     if (p.row_tiles == 1 && blocks < 2 * CUS) {
         parts = (3 * CUS + blocks - 1) / blocks;
@@ -396,6 +584,11 @@ CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_
     if (p.chunk < 128) p.chunk = 128;
     p.parts = (int)((max_kv + p.chunk - 1) / p.chunk);
     if (p.parts < 1) p.parts = 1;
+    // a workgroup takes a run of row blocks while that leaves a dozen of them per compute unit
+    p.run_shift = block_shift;
+    if (!p.few && !backward && p.parts == 1)
+        while (p.run_shift < block_shift + 3 && (blocks >> (p.run_shift - block_shift + 1)) >= 12 * CUS) ++p.run_shift;
+    p.slots = (int)((rows >> p.run_shift) + segments);
     if (!backward) return p;
     p.kv_slots = (int)(n_kv / 128 + segments);
     const long long kv_work = n_kv / 128 > segments ? n_kv / 128 : segments;

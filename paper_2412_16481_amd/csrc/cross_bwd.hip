@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256, 2) void k_cross_bwd_dq(CrossBwdArgs b)
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (!SPLIT) zero_rest(a.q_offsets, a.segments, a.n_q, (uint32_t)a.H * T::ROWB, b.dq, nullptr);
-    const uint32_t u = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);   // as in the forward kernel
+    const uint32_t u = piece_of(a.turn);
     const uint32_t x = u / (uint32_t)a.K;
     const int kh = (int)(u - x * a.K), slot = (int)(SPLIT ? x / (uint32_t)a.parts : x), part = SPLIT ? (int)(x - (uint32_t)slot * a.parts) : 0;
     if (slot >= a.slots) return;
@@ -223,20 +223,35 @@ __global__ __launch_bounds__(256, 2) void k_cross_bwd_dq(CrossBwdArgs b)
     }
 }
 
+// The query rows stream through LDS in stages of KStage::ROWS, three of them resident. Per tile of 32 rows a wave has 4 KS MFMAs for the
+// scores and dP (of the NEXT tile: they are issued between the exponentials of the current one) and 4 MT for the two gradients. The
+// starting accumulators of a tile are read from LDS: -lse (in the score's units) and -D of its rows, so neither costs a
+// subtraction, and rows past the end have -1e30 there: their probabilities are exactly zero.
+template <int D>
+struct KStage {
+    using T = Tile<D>;
+    static constexpr int ROWS = D == 16 ? 128 : 64;
+    static constexpr int TILES = ROWS / 32;
+    static constexpr int BYTES = ROWS * T::ROWB;      // of one operand
+    static constexpr int NBUF = 3;
+    static constexpr int LPW = ROWS * T::NC / 256;
+    static constexpr int TOTAL = NBUF * 2 * BYTES;
+};
+
 template <int D, bool SPLIT>
 __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossBwdArgs b)
 {
     using T = Tile<D>;
-    using S = BStage<D>;
+    using S = KStage<D>;
     constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF, BM = 128, SHIFT = 7;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::TOTAL];
-    __shared__ __attribute__((aligned(16))) float sl[NBUF][S::ROWS], sd[NBUF][S::ROWS];   // -lse (log2 units) and D of the staged rows
+    __shared__ __attribute__((aligned(16))) float sl[NBUF][S::ROWS], sd[NBUF][S::ROWS];
     const CrossArgs& a = b.f;
     const uint32_t sQ = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sG = sQ + NBUF * S::BYTES;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (!SPLIT) zero_rest(a.kv_offsets, a.segments, a.n_kv, (uint32_t)a.K * T::ROWB, b.dk, b.dv);
-    const uint32_t u = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    const uint32_t u = piece_of(b.kv_turn);
     const uint32_t x = u / (uint32_t)a.K;
     const int kh = (int)(u - x * a.K), slot = (int)(SPLIT ? x / (uint32_t)b.row_parts : x), part = SPLIT ? (int)(x - (uint32_t)slot * b.row_parts) : 0;
     if (slot >= b.kv_slots) return;
@@ -248,6 +263,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossB
     const int nrows = blk * BM >= kv.len ? 0 : SPLIT ? min(max(live - row0, 0), b.row_chunk) : live;
 
     const uint32_t row_bytes = (uint32_t)a.H * T::ROWB;
+    const float mul = a.s_mul, lmul = -LOG2E / a.s_mul;
     int srow[LPW];
     uint32_t scol[LPW];
 #pragma unroll
@@ -256,9 +272,17 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossB
         srow[i] = p / T::NC;
         scol[i] = ((p % T::NC) ^ T::swizzle(srow[i])) << 4;
     }
-    float nl = 0.f, ds = 0.f;                         // of row `tid` of the stage requested last
-    auto dma_stage = [&](int st) __attribute__((always_inline)) {
+    float nl = 0.f, nd = 0.f;                         // of row `tid` of the stage requested last
+    auto request = [&](int st) __attribute__((always_inline)) {
         const uint32_t to = (st % NBUF) * S::BYTES;
+        if (tid < S::ROWS) {
+            const int r = st * S::ROWS + tid, rc = row0 + min(r, nrows - 1);
+            const int q = divide(rc, a.G, a.by_g), g = rc - q * a.G;
+            const size_t at = (size_t)(qs.from + q) * a.H + kh * a.G + g;
+            const float l = a.lse[at], d = b.dsum[at];
+            nl = r < nrows ? l * lmul : -1e30f;
+            nd = -d;
+        }
 #pragma unroll
         for (int i = 0; i < LPW; ++i) {
             const int r = row0 + min(st * S::ROWS + srow[i], nrows - 1);
@@ -267,23 +291,19 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossB
             lds_dma16(reinterpret_cast<const char*>(a.q) + at, sQ + to + (wave * LPW + i) * 1024);
             lds_dma16(reinterpret_cast<const char*>(b.dout) + at, sG + to + (wave * LPW + i) * 1024);
         }
-        if (tid < S::ROWS) {
-            const int r = st * S::ROWS + tid, rc = row0 + min(r, nrows - 1);
-            const int q = divide(rc, a.G, a.by_g), g = rc - q * a.G;
-            const size_t at = (size_t)(qs.from + q) * a.H + kh * a.G + g;
-            const float l = a.lse[at], d = b.dsum[at];
-            nl = r < nrows ? -LOG2E * l : -1e30f;     // past the end: probabilities exactly zero
-            ds = d;
-        }
     };
     auto keep_sums = [&](int st) __attribute__((always_inline)) {
         if (tid < S::ROWS) {
             sl[st % NBUF][tid] = nl;
-            sd[st % NBUF][tid] = ds;
+            sd[st % NBUF][tid] = nd;
         }
     };
     const int nst = (nrows + S::ROWS - 1) / S::ROWS;
-    if (nst > 0) dma_stage(0);
+    if (nst > 0) {
+        request(0);
+        keep_sums(0);
+    }
+    if (nst > 1) request(1);
 
     const long long key = blk * BM + wave * 32 + l32;
     const bool has = key < kv.len && nrows > 0;
@@ -303,62 +323,118 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossB
     }
     uint32_t off[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) off[ks] = T::row_piece(lane, ks);
-    const uint32_t tr = T::transposed(lane);
-    const float mul = a.s_mul;
-    if (nst > 0) keep_sums(0);
+    for (int ks = 0; ks < KS; ++ks) off[ks] = sQ + T::row_piece(lane, ks);
+    constexpr uint32_t GQ = NBUF * S::BYTES;          // from a row of Q to the same of dO
+    const uint32_t tr = sQ + T::transposed(lane);
 
-    auto tile = [&](int buf, int t4) __attribute__((always_inline)) {
-        const uint32_t at = buf * S::BYTES + t4 * T::BYTES;
-        f32x16 s = f32x16{0}, dp = f32x16{0};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            U4 qf, gf;
-            qf.u = lds_read16(sQ + at + off[ks]);
-            gf.u = lds_read16(sG + at + off[ks]);
-            s = mfma(qf, kf[ks], s);
-            dp = mfma(gf, vf[ks], dp);
-        }
-        U4 p0, p1, d0, d1;
+    auto start = [&](f32x16& s, f32x16& dp, int buf, int t4) __attribute__((always_inline)) {
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
             const float4 l = *reinterpret_cast<const float4*>(&sl[buf][t4 * 32 + 8 * r4 + 4 * hf]);
             const float4 d = *reinterpret_cast<const float4*>(&sd[buf][t4 * 32 + 8 * r4 + 4 * hf]);
-            const float lv[4] = {l.x, l.y, l.z, l.w}, dd[4] = {d.x, d.y, d.z, d.w};
+            s[4 * r4] = l.x, s[4 * r4 + 1] = l.y, s[4 * r4 + 2] = l.z, s[4 * r4 + 3] = l.w;
+            dp[4 * r4] = d.x, dp[4 * r4 + 1] = d.y, dp[4 * r4 + 2] = d.z, dp[4 * r4 + 3] = d.w;
+        }
+    };
+    // One unit: P = 2^s, dS = P o dp of the current tile (at `at`) and its gradients, with the products of the next one (at `an` of
+    // buffer `nbuf`, its tile `nt`) in between
+    auto unit = [&](f32x16& s, f32x16& dp, uint32_t at, f32x16& sn, f32x16& dpn, uint32_t an, int nbuf, int nt) __attribute__((always_inline)) {
+        constexpr int EP = 16 / (2 * KS);             // elements behind each of the products
+        U4 qf[2], gf[2], p0, p1, d0, d1, x[2][4];
+        const auto prob = [&](int r) __attribute__((always_inline)) {
+            s[r] = __builtin_amdgcn_exp2f(s[r] * mul);
+            dp[r] *= s[r];
+        };
+        const auto turned = [&](int mt) __attribute__((always_inline)) {
+            const uint32_t t = tr + at;
+            read_transposed<D>(x[mt & 1][0], x[mt & 1][1], t + GQ, (t + GQ) ^ T::FLIP, mt);
+            read_transposed<D>(x[mt & 1][2], x[mt & 1][3], t, t ^ T::FLIP, mt);
+        };
+        start(sn, dpn, nbuf, nt);
+        qf[0].u = lds_read16(off[0] + an);
+        gf[0].u = lds_read16(off[0] + an + GQ);
+        F3D_SB();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = 4 * r4 + e;
-                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], mul, lv[e]));
-                dp[r] = (dp[r] - dd[e]) * s[r];
+        for (int ks = 0; ks < KS; ++ks) {
+            if (ks + 1 < KS) {
+                qf[(ks + 1) & 1].u = lds_read16(off[ks + 1] + an);
+                gf[(ks + 1) & 1].u = lds_read16(off[ks + 1] + an + GQ);
             }
+            if (ks == KS - 1) turned(0);
+            F3D_SB();
+#pragma unroll
+            for (int e = 0; e < EP; ++e) prob(2 * ks * EP + e);
+            F3D_SB();
+            sn = mfma(qf[ks & 1], kf[ks], sn);
+            F3D_SB();
+#pragma unroll
+            for (int e = 0; e < EP; ++e) prob((2 * ks + 1) * EP + e);
+            F3D_SB();
+            dpn = mfma(gf[ks & 1], vf[ks], dpn);
+            F3D_SB();
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             (&p0.u.x)[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
-            (&p1.u.x)[e] = pack_bf16(s[8 + 2 * e], s[8 + 2 * e + 1]);
             (&d0.u.x)[e] = pack_bf16(dp[2 * e], dp[2 * e + 1]);
-            (&d1.u.x)[e] = pack_bf16(dp[8 + 2 * e], dp[8 + 2 * e + 1]);
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            U4 g0, g1, q0, q1;
-            read_transposed<D>(g0, g1, sG + at + tr, (sG + at + tr) ^ T::FLIP, mt);
-            read_transposed<D>(q0, q1, sQ + at + tr, (sQ + at + tr) ^ T::FLIP, mt);
-            dv[mt] = mfma(g0, p0, dv[mt]);
-            dk[mt] = mfma(q0, d0, dk[mt]);
-            dv[mt] = mfma(g1, p1, dv[mt]);
-            dk[mt] = mfma(q1, d1, dk[mt]);
+            if (mt + 1 < MT) turned(mt + 1);
+            F3D_SB();
+            dv[mt] = mfma(x[mt & 1][0], p0, dv[mt]);
+            dk[mt] = mfma(x[mt & 1][2], d0, dk[mt]);
+            F3D_SB();
+            if (mt == 0) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    (&p1.u.x)[e] = pack_bf16(s[8 + 2 * e], s[8 + 2 * e + 1]);
+                    (&d1.u.x)[e] = pack_bf16(dp[8 + 2 * e], dp[8 + 2 * e + 1]);
+                }
+                F3D_SB();
+            }
+            dv[mt] = mfma(x[mt & 1][1], p1, dv[mt]);
+            dk[mt] = mfma(x[mt & 1][3], d1, dk[mt]);
+            F3D_SB();
         }
     };
-    for (int st = 0; st < nst; ++st) {
+    // Stage st + 1 is handed over to the readers and the buffer of stage st - 1 requested again for st + 2: whoever arrives has its own
+    // loads of st + 1 and has read the last of st - 1.
+    auto handover = [&](int st) __attribute__((always_inline)) {
+        if (st + 1 < nst) keep_sums(st + 1);
         __builtin_amdgcn_s_waitcnt(vm_wait(0));
         __syncthreads();
-        if (st + 1 < nst) dma_stage(st + 1);
-        if (busy) {
-#pragma unroll 1
-            for (int t4 = 0; t4 < S::TILES && st * S::ROWS + t4 * 32 < nrows; ++t4) tile(st % NBUF, t4);
+        if (st + 2 < nst) request(st + 2);
+    };
+
+    if (nst > 0) {
+        __builtin_amdgcn_s_waitcnt(vm_wait(0));       // stage 0 is here, and with it stage 1
+        __syncthreads();
+        f32x16 sa, da, sb, db;
+        start(sa, da, 0, 0);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            U4 qf, gf;
+            qf.u = lds_read16(off[ks]);
+            gf.u = lds_read16(off[ks] + GQ);
+            sa = mfma(qf, kf[ks], sa);
+            da = mfma(gf, vf[ks], da);
         }
-        if (st + 1 < nst) keep_sums(st + 1);          // its buffer was read before the barrier above
+        for (int st = 0, buf = 0; st < nst; ++st) {
+            const int bufn = buf + 1 == NBUF ? 0 : buf + 1;
+            const uint32_t at = buf * S::BYTES, an = bufn * S::BYTES;
+#pragma unroll
+            for (int t4 = 0; t4 < S::TILES; t4 += 2) {
+                if (busy) unit(sa, da, at + t4 * T::BYTES, sb, db, at + (t4 + 1) * T::BYTES, buf, t4 + 1);
+                if (t4 + 2 < S::TILES) {
+                    if (busy) unit(sb, db, at + (t4 + 1) * T::BYTES, sa, da, at + (t4 + 2) * T::BYTES, buf, t4 + 2);
+                } else {
+                    handover(st);                     // what is computed ahead of the last tile of all reads some buffer and is never used
+                    if (busy) unit(sb, db, at + (t4 + 1) * T::BYTES, sa, da, an, bufn, 0);
+                }
+            }
+            buf = bufn;
+        }
     }
     if (key >= kv.span) return;
     const size_t at = ((size_t)(kv.from + key) * a.K + kh) * D, all = (size_t)a.n_kv * a.K * D;
@@ -400,7 +476,7 @@ hipError_t launch(const CrossBwdArgs& b, hipStream_t stream)
     const CrossArgs& a = b.f;
     hipError_t e;
     if (a.n_q > 0) {
-        const unsigned grid = (unsigned)(((long long)a.slots * a.K * a.parts + 7) / 8 * 8);
+        const unsigned grid = cross_grid((long long)a.slots * a.parts, a.K, a.turn);
         constexpr int QT2 = D <= 32 ? 2 : 1;
         if (a.parts > 1) k_cross_bwd_dq<D, 1, true><<<grid, 256, 0, stream>>>(b);
         else if (a.row_tiles == 2) k_cross_bwd_dq<D, QT2, false><<<grid, 256, 0, stream>>>(b);
@@ -416,7 +492,7 @@ hipError_t launch(const CrossBwdArgs& b, hipStream_t stream)
         }
     }
     if (a.n_kv > 0) {
-        const unsigned grid = (unsigned)(((long long)b.kv_slots * a.K * b.row_parts + 7) / 8 * 8);
+        const unsigned grid = cross_grid((long long)b.kv_slots * b.row_parts, a.K, b.kv_turn);
         if (b.row_parts > 1) k_cross_bwd_dkdv<D, true><<<grid, 256, 0, stream>>>(b);
         else k_cross_bwd_dkdv<D, false><<<grid, 256, 0, stream>>>(b);
         e = hipGetLastError();

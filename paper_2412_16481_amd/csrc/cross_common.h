@@ -69,6 +69,15 @@ __device__ __forceinline__ int segment_of(const int32_t* offsets, int n, int seg
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// Which piece of work is this workgroup's. Workgroups go to the eight XCDs in turn; each XCD takes `turn` consecutive pieces, then the
+// next eight turns follow: neighbours, which read the same keys (or rows), share an L2, and segments of different lengths are still
+// spread over all of them. (One eighth of all pieces to each XCD: 16 ragged segments, 64 channels, TAG_US.)
+__device__ __forceinline__ uint32_t piece_of(uint32_t turn)
+{
+    const uint32_t i = blockIdx.x >> 3, round = i / turn;
+    return (round * 8 + (blockIdx.x & 7)) * turn + (i - round * turn);
+}
+
 // Rows of one head in LDS: row-major, the 16-byte pieces of a row xor-swizzled by the row, so that neither 16 rows read at one
 // piece nor the four rows x 64 bytes of a transposing read meet in a bank (256 bytes of them).
 template <int D>

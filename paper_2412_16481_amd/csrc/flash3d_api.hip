@@ -702,9 +702,11 @@ static int fill_cross_args(f3d::CrossArgs& a, const CrossSizes& s, const f3d::Cr
     a.f16 = f16;
     a.few = p.few;
     a.row_tiles = p.row_tiles;
+    a.run_shift = p.run_shift;
     a.slots = p.slots;
     a.parts = p.parts;
     a.chunk = p.chunk;
+    a.turn = f3d::cross_turn((long long)p.slots * p.parts, a.K);
     *scale_out = scale;
     return F3D_OK;
 }
@@ -821,6 +823,7 @@ int f3d_cross_attn_bwd(const void* q, const void* k, const void* v, const void* 
     b.part_dq = (float*)((char*)workspace + dsum);
     b.part_dkv = (float*)((char*)workspace + dsum + part);
     b.kv_slots = p.kv_slots;
+    b.kv_turn = f3d::cross_turn((long long)p.kv_slots * p.row_parts, b.f.K);
     b.row_parts = p.row_parts;
     b.row_chunk = p.row_chunk;
     (void)hipGetLastError();
