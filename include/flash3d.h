@@ -286,9 +286,9 @@ int f3d_bucket_swin_attn_bwd(const void *q, const void *k, const void *v, const 
  *               segment and behind the last keep what they held
  *   workspace   >= f3d_cross_attn_workspace_bytes(...) of the same sizes, 256-byte aligned; may be NULL where that is 0
  * Inconsistent offsets or lengths give unspecified results but no access out of bounds. out overlaps no input.
- * Arithmetic: 16-bit operands, fp32 accumulation and softmax (the running maximum followed within 2^8), the sum of the exponentials
- * taken in fp32, the probabilities rounded to 16 bits before the product with v; one rounding of the result. Inputs must be finite, and
- * so must their scaled scores in binary32. The same call gives the same bits; how the keys are split follows from n_q, n_segments,
+ * Arithmetic: 16-bit operands, fp32 accumulation and softmax, the sum of the exponentials taken in fp32, the probabilities rounded to 16
+ * bits before the product with v; one rounding of the result. Inputs must be finite, and so must the products q k^T and their scaled
+ * values in binary32. The same call gives the same bits; how the keys are split follows from n_q, n_segments,
  * max_q, max_kv, heads, kv_heads and head_dim.
  */
 int f3d_cross_attn_workspace_bytes(int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q, int64_t max_kv, int32_t heads,

@@ -19,8 +19,7 @@ struct CrossArgs {
     int segments;
     int H, K, G;                // heads, key/value heads, heads that share one of these
     Divide by_g;                // rows of a segment, heads that share keys counted one by one, by G
-    float q_pow2;               // bfloat16: a power of two, at most 1, that goes into the query (exactly), and
-    float s_mul;                // what is left of scale * log2(e), multiplied onto the score
+    float s_mul;                // softmax scale * log2(e), multiplied onto the product
     uint16_t* out;
     float* lse;                 // null, or [n_q, H]
     int f16;
@@ -32,7 +31,8 @@ struct CrossArgs {
     int parts;                  // parts the keys of a segment are split into
     int chunk;                  // keys of a part
     float* part_o;              // [parts][n_q * H][head_dim], sums of a part relative to its largest score
-    float2* part_ml;            // [parts][n_q * H]: that score (log2 units), sum of exponentials
+    float2* part_ml;            // [parts][n_q * H]: that score (log2 units), sum of the rounded exponentials
+    float* part_l;              // [parts][n_q * H]: their sum as they are, where lse is wanted
 };
 
 // consecutive pieces (row blocks x parts x key/value heads) to an XCD: the heads of up to eight blocks; the grid is whole rounds of eight turns

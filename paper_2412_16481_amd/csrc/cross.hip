@@ -18,6 +18,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "cross_common.h"
 
 namespace f3d {
@@ -39,7 +41,7 @@ struct RowStage {
     static constexpr int TOTAL = NBUF * 2 * BYTES;
 };
 
-template <int D, int QT, bool F16, bool SPLIT>
+template <int D, int QT, bool F16, bool SPLIT, bool LSE>
 __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs a)
 {
     using T = Tile<D>;
@@ -60,9 +62,10 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
     const int b = segment_of(a.q_offsets, a.n_q, a.segments, a.G, a.run_shift, slot);
     const Rows qs = rows_of(a.q_offsets, a.q_lens, a.n_q, b), kv = rows_of(a.kv_offsets, a.kv_lens, a.n_kv, b);
     const long long run = slot - first_slot(a.q_offsets, a.n_q, b, a.G, a.run_shift);
-    const long long rows = (long long)qs.span * a.G, live = (long long)qs.len * a.G, first_row = run << a.run_shift;
-    if (run < 0 || first_row >= rows) return;
-    const int blocks = (int)((min(rows, first_row + (1ll << a.run_shift)) - first_row + BM - 1) / BM);
+    const int rows = qs.span * a.G, live = qs.len * a.G;   // n_q * heads is below 2^31 by more than a run
+    if (run < 0 || (run << a.run_shift) >= rows) return;
+    const int first_row = (int)(run << a.run_shift);
+    const int blocks = (min(rows - first_row, 1 << a.run_shift) + BM - 1) / BM;
     const int key0 = SPLIT ? part * a.chunk : 0;
     const int nkeys = first_row >= live ? 0 : SPLIT ? min(max(kv.len - key0, 0), a.chunk) : kv.len;   // this workgroup's
 
@@ -89,7 +92,7 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
     };
     const int nst = (nkeys + S::ROWS - 1) / S::ROWS;
     const bool stays = nst <= NBUF;                   // all keys are resident: staged once, and no barrier behind the first
-    const int total = stays ? nst : nst * blocks;     // stages to come, over all row blocks
+    int total = stays ? nst : nst * blocks;           // stages to come, over all row blocks
     int asked = 0, ask_st = 0;                        // stages requested, the next one's keys
     auto request_next = [&](int buf) __attribute__((always_inline)) {
         request(ask_st, buf);
@@ -108,17 +111,16 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
 
     // this lane's rows: row l32 of each of the wave's tiles
     U4 qf[QT][KS];
-    auto row_of = [&](int blk, int t) __attribute__((always_inline)) { return first_row + (long long)blk * BM + wave * 32 * QT + t * 32 + l32; };
-    auto place_of = [&](long long row) __attribute__((always_inline)) {   // (query, head) of the tensor; past the end: of the last row
-        const int r = (int)min(row, rows - 1), i = divide(r, a.G, a.by_g), g = r - i * a.G;
-        return (size_t)(qs.from + i) * a.H + kh * a.G + g;
-    };
+    auto row_of = [&](int blk, int t) __attribute__((always_inline)) { return first_row + blk * BM + wave * 32 * QT + t * 32 + l32; };
+    uint32_t place[QT];                               // (query, head) of the tensor
     auto fetch_rows = [&](int blk) __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const uint16_t* const from = a.q + place_of(row_of(blk, t)) * D + hf * 8;
+            const int r = min(row_of(blk, t), rows - 1), i = divide(r, a.G, a.by_g), g = r - i * a.G;   // past the end: the last row
+            place[t] = (uint32_t)(qs.from + i) * (uint32_t)a.H + (uint32_t)(kh * a.G + g);
+            const char* const from = reinterpret_cast<const char*>(a.q) + (uint64_t)place[t] * T::ROWB + hf * 16;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) qf[t][ks].u = *reinterpret_cast<const uint4*>(from + ks * 16);
+            for (int ks = 0; ks < KS; ++ks) qf[t][ks].u = *reinterpret_cast<const uint4*>(from + ks * 32);
         }
     };
     fetch_rows(0);
@@ -128,14 +130,15 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
     }
 
     f32x16 o[QT][MT], sa, sb;
-    float m[QT], l[QT];                               // reference of the exponentials (log2 units), their sum over this lane's keys
-    U4 kf[KS];
+    float m[QT], l[QT], lr[QT];                       // reference of the exponentials (log2 units), sums over this lane's keys: as they are
+    U4 kf[KS];                                        // (for the log-sum-exp) and rounded, as the product with v takes them
     auto read_k = [&](U4 (&f)[KS], uint32_t at) __attribute__((always_inline)) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) f[ks].u = lds_read16(koff[ks] + at);
     };
     // One unit of the pipeline: the softmax of the score tile `s` (row tile t, keys from kbase on) and O^T += V^T P^T from the keys at
     // `at`, with the MFMAs of the NEXT score tile (`sn`, rows of tile tn, keys in kf) in between.
+    bool robust = false;
     auto unit = [&](f32x16& s, int t, uint32_t at, int kbase, f32x16& sn, int tn) __attribute__((always_inline)) {
         U4 p0, p1, v0[2], v1[2];
         if (kbase + 32 > nkeys) {                     // the last tile may be short
@@ -143,20 +146,23 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
             for (int r = 0; r < 16; ++r)
                 if (kbase + 8 * (r >> 2) + 4 * hf + (r & 3) >= nkeys) s[r] = -INFINITY;
         }
-        float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
+        if (robust) {                                 // the running maximum
+            float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
-        for (int r = 3; r < 15; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
-        mx = fmaxf(mx, s[15]);
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);   // the row's other keys
-        mx = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1])) * mul;
-        if (__builtin_amdgcn_ballot_w64(mx > m[t] + 8.0f)) {
-            const float top = fmaxf(m[t], mx), alpha = __builtin_amdgcn_exp2f(m[t] - top);   // the first time 2^-inf, onto zeros
-            m[t] = top;
-            l[t] *= alpha;
+            for (int r = 3; r < 15; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
+            mx = fmaxf(mx, s[15]);
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);   // the row's other keys
+            mx = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1])) * mul;
+            if (__builtin_amdgcn_ballot_w64(mx > m[t] + 8.0f)) {
+                const float top = fmaxf(m[t], mx), alpha = __builtin_amdgcn_exp2f(m[t] - top);   // the first time 2^-inf, onto zeros
+                m[t] = top;
+                if (LSE) l[t] *= alpha;
+                lr[t] *= alpha;
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
+                for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) o[t][mt][r] *= alpha;
+                    for (int r = 0; r < 16; ++r) o[t][mt][r] *= alpha;
+                }
             }
         }
         const auto prob = [&](int r) __attribute__((always_inline)) { s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], mul, -m[t])); };
@@ -172,7 +178,10 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
             F3D_SB();
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) (&p0.u.x)[e] = E::pack(s[2 * e], s[2 * e + 1]);
+        for (int e = 0; e < 4; ++e) {
+            (&p0.u.x)[e] = E::pack(s[2 * e], s[2 * e + 1]);
+            lr[t] = E::sum2((&p0.u.x)[e], lr[t]);
+        }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             if (mt + 1 < MT) read_transposed<D>(v0[(mt + 1) & 1], v1[(mt + 1) & 1], voff + at, (voff + at) ^ T::FLIP, mt + 1);
@@ -181,40 +190,35 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
             F3D_SB();
             if (mt == 0) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) (&p1.u.x)[e] = E::pack(s[8 + 2 * e], s[8 + 2 * e + 1]);
+                for (int e = 0; e < 4; ++e) {
+                    (&p1.u.x)[e] = E::pack(s[8 + 2 * e], s[8 + 2 * e + 1]);
+                    lr[t] = E::sum2((&p1.u.x)[e], lr[t]);
+                }
             }
             F3D_SB();
             o[t][mt] = E::mfma(v1[mt & 1], p1, o[t][mt]);
             F3D_SB();
 #pragma unroll
-            for (int r = mt * (16 / MT); r < (mt + 1) * (16 / MT); ++r) l[t] += s[r];
+            for (int r = mt * (16 / MT); LSE && r < (mt + 1) * (16 / MT); ++r) l[t] += s[r];
         }
     };
 
     int buf = 0;
-    for (int blk = 0; blk < blocks; ++blk) {
-        const bool busy = first_row + (long long)blk * BM + wave * 32 * QT < live;   // this wave has rows with results
-        if (!F16) {
-#pragma unroll
-            for (int t = 0; t < QT; ++t) {
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) qf[t][ks] = scale_pow2(qf[t][ks], a.q_pow2);
-            }
-        }
+    // One sweep over the keys for the block of rows in qf. The optimistic one takes the exponentials against the fixed reference 0: exact
+    // as long as the sum stays well inside the range of the formats, which is looked at afterwards.
+    auto sweep = [&](bool busy) __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            m[t] = -INFINITY;
-            l[t] = 0.f;
+            m[t] = robust ? -INFINITY : 0.f;
+            l[t] = lr[t] = 0.f;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) o[t][mt] = f32x16{0};
         }
         if (stays) buf = 0;
-        if (nst > 0) {
-            read_k(kf, buf * S::BYTES);
-            sa = f32x16{0};
+        read_k(kf, buf * S::BYTES);
+        sa = f32x16{0};
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) sa = E::mfma(kf[ks], qf[0][ks], sa);
-        }
+        for (int ks = 0; ks < KS; ++ks) sa = E::mfma(kf[ks], qf[0][ks], sa);
         for (int st = 0; st < nst; ++st) {
             const int bufn = buf + 1 == NBUF ? 0 : buf + 1;
             const uint32_t at0 = buf * S::BYTES, an0 = bufn * S::BYTES;
@@ -242,25 +246,55 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
             }
             buf = bufn;
         }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(lr[t]), __float_as_int(lr[t]), false, false);
+            lr[t] = __int_as_float(sw[0]) + __int_as_float(sw[1]);
+            if (!LSE) continue;
+            const auto su = __builtin_amdgcn_permlane32_swap(__float_as_int(l[t]), __float_as_int(l[t]), false, false);
+            l[t] = __int_as_float(su[0]) + __int_as_float(su[1]);
+        }
+    };
+    for (int blk = 0; blk < blocks; ++blk) {
+        const bool busy = first_row + blk * BM + wave * 32 * QT < live;   // this wave has rows with results
+        robust = false;
+        while (nst > 0) {
+            sweep(busy);
+            if (robust) break;
+            bool bad = false;
+#pragma unroll
+            for (int t = 0; t < QT; ++t) bad = bad || (row_of(blk, t) < live && !(lr[t] > E::SUM_LO && lr[t] < E::SUM_HI));
+            // keys that stay: every wave for itself
+            robust = stays ? __builtin_amdgcn_ballot_w64(bad) != 0 : __syncthreads_or(bad) != 0;
+            if (!robust) break;
+            if (stays) continue;
+            // the same keys once more: what is on its way for the next block are their first stages
+            total += nst;
+            if (blk + 1 == blocks) {                  // nothing is: all stages asked for have been read
+                request_next(buf);
+                if (asked < total) request_next(buf + 1 == NBUF ? 0 : buf + 1);
+                __builtin_amdgcn_s_waitcnt(vm_wait(0));
+                __syncthreads();
+            }
+        }
         // ---- results; the next block's rows are on their way meanwhile
-        size_t at_q[QT];
+        uint32_t at_q[QT];
         bool mine[QT], has[QT];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const long long row = row_of(blk, t);
+            const int row = row_of(blk, t);
             mine[t] = row < rows;
             has[t] = row < live && nkeys > 0;
-            at_q[t] = place_of(row);
+            at_q[t] = place[t];
         }
         if (blk + 1 < blocks) fetch_rows(blk + 1);
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(l[t]), __float_as_int(l[t]), false, false);
-            l[t] = __int_as_float(sw[0]) + __int_as_float(sw[1]);
             if (!mine[t]) continue;
             if (SPLIT) {
                 const size_t pa = (size_t)part * a.n_q * a.H + at_q[t];
-                if (hf == 0) a.part_ml[pa] = has[t] ? make_float2(m[t], l[t]) : make_float2(-INFINITY, 0.f);
+                if (hf == 0) a.part_ml[pa] = has[t] ? make_float2(m[t], lr[t]) : make_float2(-INFINITY, 0.f);
+                if (LSE && hf == 0) a.part_l[pa] = has[t] ? l[t] : 0.f;
                 if (!has[t]) continue;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
@@ -271,9 +305,9 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
                 }
                 continue;
             }
-            const float inv = 1.0f / l[t];
-            if (a.lse && hf == 0) a.lse[at_q[t]] = has[t] ? (m[t] + __log2f(l[t])) * LN2 : -INFINITY;
-            uint16_t* const to = a.out + at_q[t] * D;
+            const float inv = 1.0f / lr[t];
+            if (LSE && hf == 0) a.lse[at_q[t]] = has[t] ? (m[t] + __log2f(l[t])) * LN2 : -INFINITY;
+            uint16_t* const to = a.out + (size_t)at_q[t] * D;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -360,7 +394,6 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             qf[ks].u = *reinterpret_cast<const uint4*>(from + ks * 16);
-            if (!F16) qf[ks] = scale_pow2(qf[ks], a.q_pow2);
         }
     }
     uint32_t koff[KS];
@@ -370,7 +403,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a
     const float mul = a.s_mul;
 
     f32x16 o[MT];
-    float m = -INFINITY, l = 0.f;                     // reference of the exponentials (log2 units), their sum over this lane's keys
+    float m = -INFINITY, l = 0.f, lr = 0.f;           // as in the other kernel
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) o[mt] = f32x16{0};
 
@@ -396,6 +429,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a
             const float top = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - top);   // the first time 2^-inf, onto zeros
             m = top;
             l *= alpha;
+            lr *= alpha;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -411,6 +445,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a
         for (int e = 0; e < 4; ++e) {
             (&p0.u.x)[e] = E::pack(s[2 * e], s[2 * e + 1]);
             (&p1.u.x)[e] = E::pack(s[8 + 2 * e], s[8 + 2 * e + 1]);
+            lr = E::sum2((&p1.u.x)[e], E::sum2((&p0.u.x)[e], lr));
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
@@ -432,17 +467,20 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a
     {
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(l), __float_as_int(l), false, false);
         l = __int_as_float(sw[0]) + __int_as_float(sw[1]);
+        const auto su = __builtin_amdgcn_permlane32_swap(__float_as_int(lr), __float_as_int(lr), false, false);
+        lr = __int_as_float(su[0]) + __int_as_float(su[1]);
     }
 
     // ---- the four waves' results meet in LDS: row by row, channels in order
     constexpr int P = D + 4;                      // floats from one row to the next
     static_assert(4 * 32 * P * 4 <= S::TOTAL, "room for the results");
     float* const meet = reinterpret_cast<float*>(smem);
-    __shared__ float sm_[4][32], sl_[4][32];
+    __shared__ float sm_[4][32], sl_[4][32], sr_[4][32];
     __syncthreads();                              // the last stage has been read
     if (hf == 0) {
         sm_[wave][l32] = m;
         sl_[wave][l32] = l;
+        sr_[wave][l32] = lr;
     }
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -460,11 +498,12 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a
     const size_t at = (size_t)(qs.from + i) * a.H + kh * a.G + g;
     const bool counts = r < live;
     const float top = fmaxf(fmaxf(sm_[0][rr], sm_[1][rr]), fmaxf(sm_[2][rr], sm_[3][rr]));
-    float w[4], sum = 0.f;
+    float w[4], sum = 0.f, rounded = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {                 // a wave without keys has -inf, and so has `top` where all have
         w[k] = sm_[k][rr] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm_[k][rr] - top);
         sum += w[k] * sl_[k][rr];
+        rounded += w[k] * sr_[k][rr];
     }
     float y[EACH];
 #pragma unroll
@@ -477,14 +516,15 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a
     if (!counts) sum = 0.f;
     if (SPLIT) {
         const size_t pa = (size_t)part * a.n_q * a.H + at;
-        if ((tid & 7) == 0) a.part_ml[pa] = make_float2(sum > 0.f ? top : -INFINITY, sum);
+        if ((tid & 7) == 0) a.part_ml[pa] = make_float2(sum > 0.f ? top : -INFINITY, rounded);
+        if (a.lse && (tid & 7) == 0) a.part_l[pa] = sum;
         if (sum > 0.f) {
 #pragma unroll
             for (int c = 0; c < EACH; c += 2) *reinterpret_cast<float2*>(a.part_o + pa * D + c0 + c) = make_float2(y[c], y[c + 1]);
         }
         return;
     }
-    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+    const float inv = sum > 0.f ? 1.0f / rounded : 0.f;
     if (a.lse && (tid & 7) == 0) a.lse[at] = sum > 0.f ? (top + __log2f(sum)) * LN2 : -INFINITY;
 #pragma unroll
     for (int c = 0; c < EACH; c += 2) {
@@ -506,7 +546,7 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a)
     if (q < offset_of(a.q_offsets, a.n_q, 0) || q >= offset_of(a.q_offsets, a.n_q, a.segments)) return;
     float top = -INFINITY;
     for (int p = 0; p < a.parts; ++p) top = fmaxf(top, a.part_ml[p * n + at].x);
-    float sum = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f, whole = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int p = 0; p < a.parts; ++p) {
         const float2 ml = a.part_ml[p * n + at];
@@ -514,13 +554,14 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a)
         const float w = __builtin_amdgcn_exp2f(ml.x - top);
         const float4 o = *reinterpret_cast<const float4*>(a.part_o + (p * n + at) * D + c);
         sum += w * ml.y;
+        if (a.lse) whole += w * a.part_l[p * n + at];
         y[0] += w * o.x;
         y[1] += w * o.y;
         y[2] += w * o.z;
         y[3] += w * o.w;
     }
     const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-    if (a.lse && c == 0) a.lse[at] = sum > 0.f ? (top + __log2f(sum)) * LN2 : -INFINITY;
+    if (a.lse && c == 0) a.lse[at] = sum > 0.f ? (top + __log2f(whole)) * LN2 : -INFINITY;
     *reinterpret_cast<uint2*>(a.out + at * D + c) =
         make_uint2(Half<F16>::pack(y[0] * inv, y[1] * inv), Half<F16>::pack(y[2] * inv, y[3] * inv));
 }
@@ -536,13 +577,17 @@ hipError_t launch(const CrossArgs& a, hipStream_t stream)
     } else if (a.row_tiles == 2) {
         if constexpr (D <= 64) {
             if (split) return hipErrorInvalidValue;   // two tiles a wave are for launches that fill the chip
-            k_cross<D, 2, F16, false><<<grid, threads, 0, stream>>>(a);
+            if (a.lse) k_cross<D, 2, F16, false, true><<<grid, threads, 0, stream>>>(a);
+            else k_cross<D, 2, F16, false, false><<<grid, threads, 0, stream>>>(a);
         } else {
             return hipErrorInvalidValue;
         }
+    } else if (split) {
+        if (a.lse) k_cross<D, 1, F16, true, true><<<grid, threads, 0, stream>>>(a);
+        else k_cross<D, 1, F16, true, false><<<grid, threads, 0, stream>>>(a);
     } else {
-        if (split) k_cross<D, 1, F16, true><<<grid, threads, 0, stream>>>(a);
-        else k_cross<D, 1, F16, false><<<grid, threads, 0, stream>>>(a);
+        if (a.lse) k_cross<D, 1, F16, false, true><<<grid, threads, 0, stream>>>(a);
+        else k_cross<D, 1, F16, false, false><<<grid, threads, 0, stream>>>(a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !split) return e;

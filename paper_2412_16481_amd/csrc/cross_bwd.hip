@@ -147,7 +147,6 @@ __global__ __launch_bounds__(256, 2) void k_cross_bwd_dq(CrossBwdArgs b)
                 dot += __uint_as_float(y << 16) * __uint_as_float(z << 16);
                 dot += __uint_as_float(y & 0xFFFF0000u) * __uint_as_float(z & 0xFFFF0000u);
             }
-            qf[t][ks] = scale_pow2(qf[t][ks], a.q_pow2);
         }
         dsum[t] = dot + __shfl_xor(dot, 32, 64);
         if (takes[t] && part == 0 && hf == 0) b.dsum[at] = dsum[t];
@@ -316,7 +315,6 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossB
         for (int ks = 0; ks < KS; ++ks) {
             kf[ks].u = *reinterpret_cast<const uint4*>(a.k + at + ks * 16);
             vf[ks].u = *reinterpret_cast<const uint4*>(a.v + at + ks * 16);
-            kf[ks] = scale_pow2(kf[ks], a.q_pow2);
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) dk[mt] = dv[mt] = f32x16{0};

@@ -10,6 +10,10 @@ namespace {
 
 template <bool F16>
 struct Half {
+    // Bounds of a sum of exponentials taken against the reference 0. bfloat16: none overflowed, and the largest is far above the
+    // flush-to-zero range. binary16: a probability above 65504 rounds to infinity, and what is lost of those below 2^-14 stays below
+    // 2^-25 a key of the sum.
+    static constexpr float SUM_LO = F16 ? 1.0f : 0x1p-40f, SUM_HI = F16 ? 65504.f : 0x1p80f;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi)
     {
         if constexpr (F16) {
@@ -19,6 +23,12 @@ struct Half {
         } else {
             return pack_bf16(lo, hi);
         }
+    }
+    static __device__ __forceinline__ float sum2(uint32_t pair, float c)   // c + both halves of the pair
+    {
+        const uint32_t ones = F16 ? 0x3C003C00u : 0x3F803F80u;
+        if constexpr (F16) return __builtin_amdgcn_fdot2(*reinterpret_cast<const f16x2*>(&pair), *reinterpret_cast<const f16x2*>(&ones), c, false);
+        else return __builtin_amdgcn_fdot2_f32_bf16(*reinterpret_cast<const bf16x2*>(&pair), *reinterpret_cast<const bf16x2*>(&ones), c, false);
     }
     static __device__ __forceinline__ f32x16 mfma(const U4& x, const U4& y, f32x16 c)
     {

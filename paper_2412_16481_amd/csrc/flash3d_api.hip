@@ -654,7 +654,7 @@ static size_t cross_part_bytes(const CrossSizes& s, const f3d::CrossPlan& p)
 
 static size_t cross_ml_bytes(const CrossSizes& s, const f3d::CrossPlan& p)
 {
-    return p.parts > 1 ? align_up((size_t)p.parts * s.n_q * s.heads * sizeof(float2), 256) : 0;
+    return p.parts > 1 ? align_up((size_t)p.parts * s.n_q * s.heads * 3 * sizeof(float), 256) : 0;   // a pair and one more
 }
 
 static f3d::CrossPlan cross_plan(const CrossSizes& s, bool backward)
@@ -689,16 +689,8 @@ static int fill_cross_args(f3d::CrossArgs& a, const CrossSizes& s, const f3d::Cr
     a.G = s.heads / s.kv_heads;
     a.by_g = f3d::make_divide(a.G, s.n_q * a.G);
     const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / sqrtf((float)s.head_dim);
-    const float c_log2 = scale * 1.44269504088896340736f;
-    a.q_pow2 = 1.0f;
-    a.s_mul = c_log2;
-    if (f16) {
-        a.s_mul = fminf(c_log2, 0x1p90f);   // as in f3d_bucket_swin_attn_f16
-    } else if (c_log2 < 1.0f) {             // c_log2 = q_pow2 * s_mul, 1 <= s_mul < 2
-        int e = 0;
-        a.s_mul = 2.0f * frexpf(c_log2, &e);
-        a.q_pow2 = ldexpf(1.0f, e - 1);
-    }
+    a.s_mul = scale * 1.44269504088896340736f;
+    if (f16) a.s_mul = fminf(a.s_mul, 0x1p90f);   // as in f3d_bucket_swin_attn_f16
     a.f16 = f16;
     a.few = p.few;
     a.row_tiles = p.row_tiles;
@@ -746,6 +738,7 @@ static int cross_forward(int f16, const void* q, const void* k, const void* v, c
         if (workspace_bytes < need) return F3D_ERR_WORKSPACE_TOO_SMALL;
         a.part_o = (float*)workspace;
         a.part_ml = (float2*)((char*)workspace + part);
+        a.part_l = (float*)(a.part_ml + (size_t)p.parts * n_q * heads);
     }
     a.out = (uint16_t*)out;
     a.lse = lse;
