@@ -24,7 +24,6 @@ struct CrossArgs {
     float* lse;                 // null, or [n_q, H]
     int f16;
     int few;                    // the form for few query rows
-    int row_tiles;              // tiles of 32 query rows a wave owns
     int run_shift;              // a workgroup takes 2^run_shift rows of a segment
     int slots;                  // such runs over all segments (upper bound, surplus workgroups exit)
     int turn;                   // consecutive pieces of work that go to one XCD
@@ -57,7 +56,7 @@ struct CrossBwdArgs {
 
 // What a call takes: a rule on sizes the host knows
 struct CrossPlan {
-    int few, row_tiles, run_shift, slots, parts, chunk;
+    int few, run_shift, slots, parts, chunk;
     int kv_slots, row_parts, row_chunk;   // backward
 };
 CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_q, long long max_kv, int heads, int kv_heads, int head_dim, bool backward);

@@ -28,27 +28,15 @@ namespace {
 
 constexpr float LN2 = 0.6931471805599453f;
 
-// Keys stream through LDS in stages, three of them resident; a wave owns QT tiles of 32 rows at a time.
-template <int D>
-struct RowStage {
-    using T = Tile<D>;
-    static constexpr int WAVES = D == 128 ? 8 : 4;    // 128: three stages leave room for one workgroup on a compute unit
-    static constexpr int ROWS = D <= 32 ? 128 : 64;
-    static constexpr int TILES = ROWS / 32;
-    static constexpr int BYTES = ROWS * T::ROWB;      // of K, and of V
-    static constexpr int NBUF = 3;
-    static constexpr int LPW = ROWS * T::NC / (64 * WAVES);
-    static constexpr int TOTAL = NBUF * 2 * BYTES;
-};
-
-template <int D, int QT, bool F16, bool SPLIT, bool LSE>
+// Many query rows: a wave owns a tile of 32 of them at a time.
+template <int D, bool F16, bool SPLIT, bool LSE>
 __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs a)
 {
     using T = Tile<D>;
     using S = RowStage<D>;
     using E = Half<F16>;
     constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF, NW = S::WAVES;
-    constexpr int BM = 32 * QT * NW;                  // rows of a workgroup at a time
+    constexpr int BM = 32 * NW;                  // rows of a workgroup at a time
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::TOTAL];
     const uint32_t sK = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sV = sK + NBUF * S::BYTES;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
@@ -101,7 +89,9 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
     };
     if (total > 0) request_next(0);
     if (total > 1) request_next(1);
-    if (stays && total > 2) request_next(2);
+#pragma unroll
+    for (int i = 2; i < NBUF; ++i)
+        if (stays && total > i) request_next(i);
 
     uint32_t koff[KS];
 #pragma unroll
@@ -109,37 +99,34 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
     const uint32_t voff = sV + T::transposed(lane);
     const float mul = a.s_mul;
 
-    // this lane's rows: row l32 of each of the wave's tiles
-    U4 qf[QT][KS];
-    auto row_of = [&](int blk, int t) __attribute__((always_inline)) { return first_row + blk * BM + wave * 32 * QT + t * 32 + l32; };
-    uint32_t place[QT];                               // (query, head) of the tensor
-    auto fetch_rows = [&](int blk) __attribute__((always_inline)) {
+    // this lane's row: row l32 of the wave's tile
+    U4 qf[KS];
+    auto row_of = [&](int blk) __attribute__((always_inline)) { return first_row + blk * BM + wave * 32 + l32; };
+    uint32_t place;                                   // (query, head) of the tensor
+    auto fetch_row = [&](int blk) __attribute__((always_inline)) {
+        const int r = min(row_of(blk), rows - 1), i = divide(r, a.G, a.by_g), g = r - i * a.G;   // past the end: the last row
+        place = (uint32_t)(qs.from + i) * (uint32_t)a.H + (uint32_t)(kh * a.G + g);
+        const char* const from = reinterpret_cast<const char*>(a.q) + (uint64_t)place * T::ROWB + hf * 16;
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            const int r = min(row_of(blk, t), rows - 1), i = divide(r, a.G, a.by_g), g = r - i * a.G;   // past the end: the last row
-            place[t] = (uint32_t)(qs.from + i) * (uint32_t)a.H + (uint32_t)(kh * a.G + g);
-            const char* const from = reinterpret_cast<const char*>(a.q) + (uint64_t)place[t] * T::ROWB + hf * 16;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) qf[t][ks].u = *reinterpret_cast<const uint4*>(from + ks * 32);
-        }
+        for (int ks = 0; ks < KS; ++ks) qf[ks].u = *reinterpret_cast<const uint4*>(from + ks * 32);
     };
-    fetch_rows(0);
+    fetch_row(0);
     if (total > 0) {
         __builtin_amdgcn_s_waitcnt(vm_wait(0));
         __syncthreads();                              // the stages asked for so far are here
     }
 
-    f32x16 o[QT][MT], sa, sb;
-    float m[QT], l[QT], lr[QT];                       // reference of the exponentials (log2 units), sums over this lane's keys: as they are
+    f32x16 o[MT], sa, sb;
+    float m, l, lr;                                   // reference of the exponentials (log2 units), sums over this lane's keys: as they are
     U4 kf[KS];                                        // (for the log-sum-exp) and rounded, as the product with v takes them
     auto read_k = [&](U4 (&f)[KS], uint32_t at) __attribute__((always_inline)) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) f[ks].u = lds_read16(koff[ks] + at);
     };
-    // One unit of the pipeline: the softmax of the score tile `s` (row tile t, keys from kbase on) and O^T += V^T P^T from the keys at
-    // `at`, with the MFMAs of the NEXT score tile (`sn`, rows of tile tn, keys in kf) in between.
+    // One unit of the pipeline: the softmax of the score tile `s` (keys from kbase on) and O^T += V^T P^T from the keys at
+    // `at`, with the MFMAs of the NEXT score tile (`sn`, keys in kf) in between.
     bool robust = false;
-    auto unit = [&](f32x16& s, int t, uint32_t at, int kbase, f32x16& sn, int tn) __attribute__((always_inline)) {
+    auto unit = [&](f32x16& s, uint32_t at, int kbase, f32x16& sn) __attribute__((always_inline)) {
         U4 p0, p1, v0[2], v1[2];
         if (kbase + 32 > nkeys) {                     // the last tile may be short
 #pragma unroll
@@ -153,19 +140,19 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
             mx = fmaxf(mx, s[15]);
             const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);   // the row's other keys
             mx = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1])) * mul;
-            if (__builtin_amdgcn_ballot_w64(mx > m[t] + 8.0f)) {
-                const float top = fmaxf(m[t], mx), alpha = __builtin_amdgcn_exp2f(m[t] - top);   // the first time 2^-inf, onto zeros
-                m[t] = top;
-                if (LSE) l[t] *= alpha;
-                lr[t] *= alpha;
+            if (__builtin_amdgcn_ballot_w64(mx > m + 8.0f)) {
+                const float top = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - top);   // the first time 2^-inf, onto zeros
+                m = top;
+                if (LSE) l *= alpha;
+                lr *= alpha;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) o[t][mt][r] *= alpha;
+                    for (int r = 0; r < 16; ++r) o[mt][r] *= alpha;
                 }
             }
         }
-        const auto prob = [&](int r) __attribute__((always_inline)) { s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], mul, -m[t])); };
+        const auto prob = [&](int r) __attribute__((always_inline)) { s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], mul, -m)); };
         constexpr int EP = 16 / KS;
         F3D_SB();
         read_transposed<D>(v0[0], v1[0], voff + at, (voff + at) ^ T::FLIP, 0);
@@ -174,32 +161,32 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
 #pragma unroll
             for (int e = 0; e < EP; ++e) prob(ks * EP + e);
             F3D_SB();
-            sn = E::mfma(kf[ks], qf[tn][ks], ks == 0 ? f32x16{0} : sn);
+            sn = E::mfma(kf[ks], qf[ks], ks == 0 ? f32x16{0} : sn);
             F3D_SB();
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             (&p0.u.x)[e] = E::pack(s[2 * e], s[2 * e + 1]);
-            lr[t] = E::sum2((&p0.u.x)[e], lr[t]);
+            lr = E::sum2((&p0.u.x)[e], lr);
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             if (mt + 1 < MT) read_transposed<D>(v0[(mt + 1) & 1], v1[(mt + 1) & 1], voff + at, (voff + at) ^ T::FLIP, mt + 1);
             F3D_SB();
-            o[t][mt] = E::mfma(v0[mt & 1], p0, o[t][mt]);
+            o[mt] = E::mfma(v0[mt & 1], p0, o[mt]);
             F3D_SB();
             if (mt == 0) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     (&p1.u.x)[e] = E::pack(s[8 + 2 * e], s[8 + 2 * e + 1]);
-                    lr[t] = E::sum2((&p1.u.x)[e], lr[t]);
+                    lr = E::sum2((&p1.u.x)[e], lr);
                 }
             }
             F3D_SB();
-            o[t][mt] = E::mfma(v1[mt & 1], p1, o[t][mt]);
+            o[mt] = E::mfma(v1[mt & 1], p1, o[mt]);
             F3D_SB();
 #pragma unroll
-            for (int r = mt * (16 / MT); LSE && r < (mt + 1) * (16 / MT); ++r) l[t] += s[r];
+            for (int r = mt * (16 / MT); LSE && r < (mt + 1) * (16 / MT); ++r) l += s[r];
         }
     };
 
@@ -207,18 +194,15 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
     // One sweep over the keys for the block of rows in qf. The optimistic one takes the exponentials against the fixed reference 0: exact
     // as long as the sum stays well inside the range of the formats, which is looked at afterwards.
     auto sweep = [&](bool busy) __attribute__((always_inline)) {
+        m = robust ? -INFINITY : 0.f;
+        l = lr = 0.f;
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            m[t] = robust ? -INFINITY : 0.f;
-            l[t] = lr[t] = 0.f;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) o[t][mt] = f32x16{0};
-        }
+        for (int mt = 0; mt < MT; ++mt) o[mt] = f32x16{0};
         if (stays) buf = 0;
         read_k(kf, buf * S::BYTES);
         sa = f32x16{0};
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) sa = E::mfma(kf[ks], qf[0][ks], sa);
+        for (int ks = 0; ks < KS; ++ks) sa = E::mfma(kf[ks], qf[ks], sa);
         for (int st = 0; st < nst; ++st) {
             const int bufn = buf + 1 == NBUF ? 0 : buf + 1;
             const uint32_t at0 = buf * S::BYTES, an0 = bufn * S::BYTES;
@@ -234,36 +218,25 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
                 const int kbase = st * S::ROWS + t4 * 32;
                 if (!busy || kbase >= nkeys) continue;
                 const uint32_t at = at0 + t4 * T::BYTES, an = t4 + 1 < S::TILES ? at + T::BYTES : an0;
-                if (QT == 1) {
-                    read_k(kf, an);                   // what is computed ahead of the last tile is never used
-                    if ((t4 & 1) == 0) unit(sa, 0, at, kbase, sb, 0);
-                    else unit(sb, 0, at, kbase, sa, 0);
-                } else {
-                    unit(sa, 0, at, kbase, sb, QT - 1);
-                    read_k(kf, an);
-                    unit(sb, QT - 1, at, kbase, sa, 0);
-                }
+                read_k(kf, an);                       // what is computed ahead of the last tile is never used
+                if ((t4 & 1) == 0) unit(sa, at, kbase, sb);
+                else unit(sb, at, kbase, sa);
             }
             buf = bufn;
         }
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(lr[t]), __float_as_int(lr[t]), false, false);
-            lr[t] = __int_as_float(sw[0]) + __int_as_float(sw[1]);
-            if (!LSE) continue;
-            const auto su = __builtin_amdgcn_permlane32_swap(__float_as_int(l[t]), __float_as_int(l[t]), false, false);
-            l[t] = __int_as_float(su[0]) + __int_as_float(su[1]);
-        }
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(lr), __float_as_int(lr), false, false);
+        lr = __int_as_float(sw[0]) + __int_as_float(sw[1]);
+        if (!LSE) return;
+        const auto su = __builtin_amdgcn_permlane32_swap(__float_as_int(l), __float_as_int(l), false, false);
+        l = __int_as_float(su[0]) + __int_as_float(su[1]);
     };
     for (int blk = 0; blk < blocks; ++blk) {
-        const bool busy = first_row + blk * BM + wave * 32 * QT < live;   // this wave has rows with results
+        const bool busy = first_row + blk * BM + wave * 32 < live;   // this wave has rows with results
         robust = false;
         while (nst > 0) {
             sweep(busy);
             if (robust) break;
-            bool bad = false;
-#pragma unroll
-            for (int t = 0; t < QT; ++t) bad = bad || (row_of(blk, t) < live && !(lr[t] > E::SUM_LO && lr[t] < E::SUM_HI));
+            const bool bad = row_of(blk) < live && !(lr > E::SUM_LO && lr < E::SUM_HI);
             // keys that stay: every wave for itself
             robust = stays ? __builtin_amdgcn_ballot_w64(bad) != 0 : __syncthreads_or(bad) != 0;
             if (!robust) break;
@@ -278,47 +251,38 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
             }
         }
         // ---- results; the next block's rows are on their way meanwhile
-        uint32_t at_q[QT];
-        bool mine[QT], has[QT];
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            const int row = row_of(blk, t);
-            mine[t] = row < rows;
-            has[t] = row < live && nkeys > 0;
-            at_q[t] = place[t];
-        }
-        if (blk + 1 < blocks) fetch_rows(blk + 1);
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            if (!mine[t]) continue;
-            if (SPLIT) {
-                const size_t pa = (size_t)part * a.n_q * a.H + at_q[t];
-                if (hf == 0) a.part_ml[pa] = has[t] ? make_float2(m[t], lr[t]) : make_float2(-INFINITY, 0.f);
-                if (LSE && hf == 0) a.part_l[pa] = has[t] ? l[t] : 0.f;
-                if (!has[t]) continue;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-                    for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4)
-                        *reinterpret_cast<float4*>(a.part_o + pa * D + mt * 32 + 8 * r4 + 4 * hf) =
-                            make_float4(o[t][mt][4 * r4], o[t][mt][4 * r4 + 1], o[t][mt][4 * r4 + 2], o[t][mt][4 * r4 + 3]);
-                }
-                continue;
-            }
-            const float inv = 1.0f / lr[t];
-            if (LSE && hf == 0) a.lse[at_q[t]] = has[t] ? (m[t] + __log2f(l[t])) * LN2 : -INFINITY;
-            uint16_t* const to = a.out + (size_t)at_q[t] * D;
+        const int row = row_of(blk);
+        const bool has = row < live && nkeys > 0;
+        const uint32_t at_q = place;
+        if (blk + 1 < blocks) fetch_row(blk + 1);
+        if (row >= rows) continue;
+        if (SPLIT) {
+            const size_t pa = (size_t)part * a.n_q * a.H + at_q;
+            if (hf == 0) a.part_ml[pa] = has ? make_float2(m, lr) : make_float2(-INFINITY, 0.f);
+            if (LSE && hf == 0) a.part_l[pa] = has ? l : 0.f;
+            if (!has) continue;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-                for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4) {
-                    uint2 y = make_uint2(0, 0);
-                    if (has[t]) {
-                        y.x = E::pack(o[t][mt][4 * r4] * inv, o[t][mt][4 * r4 + 1] * inv);
-                        y.y = E::pack(o[t][mt][4 * r4 + 2] * inv, o[t][mt][4 * r4 + 3] * inv);
-                    }
-                    *reinterpret_cast<uint2*>(to + mt * 32 + 8 * r4 + 4 * hf) = y;
+                for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4)
+                    *reinterpret_cast<float4*>(a.part_o + pa * D + mt * 32 + 8 * r4 + 4 * hf) =
+                        make_float4(o[mt][4 * r4], o[mt][4 * r4 + 1], o[mt][4 * r4 + 2], o[mt][4 * r4 + 3]);
+            }
+            continue;
+        }
+        const float inv = 1.0f / lr;
+        if (LSE && hf == 0) a.lse[at_q] = has ? (m + __log2f(l)) * LN2 : -INFINITY;
+        uint16_t* const to = a.out + (size_t)at_q * D;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int r4 = 0; r4 < (D == 16 ? 2 : 4); ++r4) {
+                uint2 y = make_uint2(0, 0);
+                if (has) {
+                    y.x = E::pack(o[mt][4 * r4] * inv, o[mt][4 * r4 + 1] * inv);
+                    y.y = E::pack(o[mt][4 * r4 + 2] * inv, o[mt][4 * r4 + 3] * inv);
                 }
+                *reinterpret_cast<uint2*>(to + mt * 32 + 8 * r4 + 4 * hf) = y;
             }
         }
     }
@@ -574,20 +538,12 @@ hipError_t launch(const CrossArgs& a, hipStream_t stream)
     if (a.few) {
         if (split) k_cross_few<D, F16, true><<<grid, 256, 0, stream>>>(a);
         else k_cross_few<D, F16, false><<<grid, 256, 0, stream>>>(a);
-    } else if (a.row_tiles == 2) {
-        if constexpr (D <= 64) {
-            if (split) return hipErrorInvalidValue;   // two tiles a wave are for launches that fill the chip
-            if (a.lse) k_cross<D, 2, F16, false, true><<<grid, threads, 0, stream>>>(a);
-            else k_cross<D, 2, F16, false, false><<<grid, threads, 0, stream>>>(a);
-        } else {
-            return hipErrorInvalidValue;
-        }
     } else if (split) {
-        if (a.lse) k_cross<D, 1, F16, true, true><<<grid, threads, 0, stream>>>(a);
-        else k_cross<D, 1, F16, true, false><<<grid, threads, 0, stream>>>(a);
+        if (a.lse) k_cross<D, F16, true, true><<<grid, threads, 0, stream>>>(a);
+        else k_cross<D, F16, true, false><<<grid, threads, 0, stream>>>(a);
     } else {
-        if (a.lse) k_cross<D, 1, F16, false, true><<<grid, threads, 0, stream>>>(a);
-        else k_cross<D, 1, F16, false, false><<<grid, threads, 0, stream>>>(a);
+        if (a.lse) k_cross<D, F16, false, true><<<grid, threads, 0, stream>>>(a);
+        else k_cross<D, F16, false, false><<<grid, threads, 0, stream>>>(a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !split) return e;
@@ -611,15 +567,13 @@ CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_
     CrossPlan p = {};
     const long long rows = n_q * group;               // of one key/value head
     p.few = max_q * group <= 32 && !backward;
-    p.row_tiles = !p.few && head_dim <= (backward ? 32 : 64) && (rows / 256) * kv_heads >= 2 * CUS ? 2 : 1;
-    int block_shift = p.few ? 5 : 7 + (p.row_tiles == 2);
-    if (head_dim == 128 && !p.few && !backward) block_shift = 8;   // eight waves
+    const int block_shift = p.few ? 5 : head_dim == 128 ? 8 : 7;   // one wave's tile, or that of eight or four waves
     // fewer than two workgroups per compute unit: parts of 256 keys at least, until there are about three
     long long work = (rows + (1ll << block_shift) - 1) >> block_shift;
     if (work < segments) work = segments;
     const long long blocks = work * kv_heads;
     long long parts = 1;
-    if (p.row_tiles == 1 && blocks < 2 * CUS) {
+    if (blocks < 2 * CUS) {
         parts = (3 * CUS + blocks - 1) / blocks;
         const long long most = (max_kv + 255) / 256;
         if (parts > most) parts = most;
@@ -631,7 +585,7 @@ CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_
     if (p.parts < 1) p.parts = 1;
     // a workgroup takes a run of row blocks while that leaves a dozen of them per compute unit
     p.run_shift = block_shift;
-    if (!p.few && !backward && p.parts == 1)
+    if (!p.few && p.parts == 1)
         while (p.run_shift < block_shift + 3 && (blocks >> (p.run_shift - block_shift + 1)) >= 12 * CUS) ++p.run_shift;
     p.slots = (int)((rows >> p.run_shift) + segments);
     if (!backward) return p;

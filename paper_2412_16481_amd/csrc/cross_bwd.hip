@@ -23,17 +23,6 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
 
-template <int D>
-struct BStage {
-    using T = Tile<D>;
-    static constexpr int ROWS = D == 128 ? 64 : 128;
-    static constexpr int TILES = ROWS / 32;
-    static constexpr int BYTES = ROWS * T::ROWB;      // of one operand
-    static constexpr int NBUF = 2;
-    static constexpr int LPW = ROWS * T::NC / 256;
-    static constexpr int TOTAL = NBUF * 2 * BYTES;
-};
-
 __device__ __forceinline__ f32x16 mfma(const U4& x, const U4& y, f32x16 c)
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.b, y.b, c, 0, 0, 0);
@@ -62,23 +51,26 @@ __device__ __forceinline__ void zero_rest(const int32_t* offsets, int segments, 
     const int before = offset_of(offsets, n, 0), from = offset_of(offsets, n, segments);
     if (before == 0 && from == n) return;
     const long long head = (long long)min(before, from) * row_bytes / 16, tail = (long long)from * row_bytes / 16, all = (long long)n * row_bytes / 16;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < head + all - tail; i += (long long)gridDim.x * 256) {
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < head + all - tail; i += (long long)gridDim.x * blockDim.x) {
         const long long at = i < head ? i : tail + (i - head);
         reinterpret_cast<uint4*>(x)[at] = make_uint4(0, 0, 0, 0);
         if (y) reinterpret_cast<uint4*>(y)[at] = make_uint4(0, 0, 0, 0);
     }
 }
 
-template <int D, int QT, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void k_cross_bwd_dq(CrossBwdArgs b)
+// Runs of row blocks, stages and their hand-over as in the forward kernel. Per tile of 32 keys a wave has 2 KS MFMAs for the scores and dP
+// (of the NEXT tile, issued between the exponentials of the current one; -D is the accumulator dP starts from) and 2 MT for dQ.
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross_bwd_dq(CrossBwdArgs b)
 {
     using T = Tile<D>;
-    using S = BStage<D>;
-    constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF;
-    constexpr int BM = 128 * QT, SHIFT = QT == 2 ? 8 : 7;
+    using S = RowStage<D>;
+    constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF, NW = S::WAVES;
+    constexpr int BM = 32 * NW;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::TOTAL];
     const CrossArgs& a = b.f;
-    const uint32_t sK = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sV = sK + NBUF * S::BYTES;
+    const uint32_t sK = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+    constexpr uint32_t KV = NBUF * S::BYTES;          // from a row of K to the same of V
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (!SPLIT) zero_rest(a.q_offsets, a.segments, a.n_q, (uint32_t)a.H * T::ROWB, b.dq, nullptr);
@@ -86,13 +78,15 @@ __global__ __launch_bounds__(256, 2) void k_cross_bwd_dq(CrossBwdArgs b)
     const uint32_t x = u / (uint32_t)a.K;
     const int kh = (int)(u - x * a.K), slot = (int)(SPLIT ? x / (uint32_t)a.parts : x), part = SPLIT ? (int)(x - (uint32_t)slot * a.parts) : 0;
     if (slot >= a.slots) return;
-    const int seg = segment_of(a.q_offsets, a.n_q, a.segments, a.G, SHIFT, slot);
+    const int seg = segment_of(a.q_offsets, a.n_q, a.segments, a.G, a.run_shift, slot);
     const Rows qs = rows_of(a.q_offsets, a.q_lens, a.n_q, seg), kv = rows_of(a.kv_offsets, a.kv_lens, a.n_kv, seg);
-    const long long blk = slot - first_slot(a.q_offsets, a.n_q, seg, a.G, SHIFT);
-    const long long rows = (long long)qs.span * a.G, live = (long long)qs.len * a.G;
-    if (blk < 0 || blk * BM >= rows) return;
+    const long long run = slot - first_slot(a.q_offsets, a.n_q, seg, a.G, a.run_shift);
+    const int rows = qs.span * a.G, live = qs.len * a.G;
+    if (run < 0 || (run << a.run_shift) >= rows) return;
+    const int first_row = (int)(run << a.run_shift);
+    const int blocks = (min(rows - first_row, 1 << a.run_shift) + BM - 1) / BM;
     const int key0 = SPLIT ? part * a.chunk : 0;
-    const int nkeys = blk * BM >= live ? 0 : SPLIT ? min(max(kv.len - key0, 0), a.chunk) : kv.len;
+    const int nkeys = first_row >= live ? 0 : SPLIT ? min(max(kv.len - key0, 0), a.chunk) : kv.len;
 
     const uint32_t row_bytes = (uint32_t)a.K * T::ROWB;
     const uint64_t first = (uint64_t)(kv.from + key0) * row_bytes + (uint64_t)kh * T::ROWB;
@@ -104,121 +98,174 @@ __global__ __launch_bounds__(256, 2) void k_cross_bwd_dq(CrossBwdArgs b)
         srow[i] = p / T::NC;
         scol[i] = ((p % T::NC) ^ T::swizzle(srow[i])) << 4;
     }
-    auto dma_stage = [&](int st) __attribute__((always_inline)) {
-        const uint32_t to = (st % NBUF) * S::BYTES;
+    const int nst = (nkeys + S::ROWS - 1) / S::ROWS;
+    const bool stays = nst <= NBUF;
+    const int total = stays ? nst : nst * blocks;
+    int asked = 0, ask_st = 0;
+    auto request_next = [&](int buf) __attribute__((always_inline)) {
+        const uint32_t to = buf * S::BYTES;
 #pragma unroll
         for (int i = 0; i < LPW; ++i) {
-            const int key = min(st * S::ROWS + srow[i], nkeys - 1);
+            const int key = min(ask_st * S::ROWS + srow[i], nkeys - 1);
             const uint64_t at = first + (uint64_t)(uint32_t)key * row_bytes + scol[i];
             lds_dma16(reinterpret_cast<const char*>(a.k) + at, sK + to + (wave * LPW + i) * 1024);
-            lds_dma16(reinterpret_cast<const char*>(a.v) + at, sV + to + (wave * LPW + i) * 1024);
+            lds_dma16(reinterpret_cast<const char*>(a.v) + at, sK + KV + to + (wave * LPW + i) * 1024);
         }
+        ++asked;
+        ask_st = ask_st + 1 == nst ? 0 : ask_st + 1;
     };
-    const int nst = (nkeys + S::ROWS - 1) / S::ROWS;
-    if (nst > 0) dma_stage(0);
+    if (total > 0) request_next(0);
+    if (total > 1) request_next(1);
+#pragma unroll
+    for (int i = 2; i < NBUF; ++i)
+        if (stays && total > i) request_next(i);
 
-    U4 qf[QT][KS], gf[QT][KS];
-    long long row[QT];
-    size_t at_q[QT];
-    bool takes[QT];
-    float nl[QT], dsum[QT];
-    f32x16 acc[QT][MT];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        row[t] = blk * BM + wave * 32 * QT + t * 32 + l32;
-        const int r = (int)min(row[t], max(live, 1ll) - 1);   // past the end, or behind the segment's length: a row that counts, dropped
-        const int i = divide(r, a.G, a.by_g), g = r - i * a.G;
-        const size_t at = (size_t)(qs.from + i) * a.H + kh * a.G + g;
-        takes[t] = row[t] < live;
-        const int ro = (int)min(row[t], rows - 1), io = divide(ro, a.G, a.by_g);
-        at_q[t] = (size_t)(qs.from + io) * a.H + kh * a.G + (ro - io * a.G);
-        if (row[t] >= rows) row[t] = -1;
-        float dot = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            U4 of;
-            const size_t from = at * D + ks * 16 + hf * 8;
-            qf[t][ks].u = *reinterpret_cast<const uint4*>(a.q + from);
-            gf[t][ks].u = *reinterpret_cast<const uint4*>(b.dout + from);
-            of.u = *reinterpret_cast<const uint4*>(a.out + from);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t y = (&of.u.x)[e], z = (&gf[t][ks].u.x)[e];
-                dot += __uint_as_float(y << 16) * __uint_as_float(z << 16);
-                dot += __uint_as_float(y & 0xFFFF0000u) * __uint_as_float(z & 0xFFFF0000u);
-            }
-        }
-        dsum[t] = dot + __shfl_xor(dot, 32, 64);
-        if (takes[t] && part == 0 && hf == 0) b.dsum[at] = dsum[t];
-        nl[t] = takes[t] && nkeys > 0 ? -LOG2E * a.lse[at] : -1e30f;   // rows that take no part: probabilities exactly zero
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) acc[t][mt] = f32x16{0};
-    }
-    const bool busy = blk * BM + wave * 32 * QT < live;
     uint32_t off[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) off[ks] = T::row_piece(lane, ks);
+    for (int ks = 0; ks < KS; ++ks) off[ks] = sK + T::row_piece(lane, ks);
     const uint32_t toff = sK + T::transposed(lane);
     const float mul = a.s_mul;
+    if (total > 0) {
+        __builtin_amdgcn_s_waitcnt(vm_wait(0));
+        __syncthreads();
+    }
 
-    auto tile = [&](uint32_t at, int kbase) __attribute__((always_inline)) {
-        U4 kf[KS], vf[KS];
-        f32x16 s[QT], dp[QT];
-        U4 p0[QT], p1[QT];
+    U4 qf[KS], gf[KS];
+    f32x16 acc[MT], minus_d;
+    float nl;
+    // One unit: dS = P o (dP - D) of the current tile (keys from kbase on, at `at`) and its dQ, with the products of the next (at `an`)
+    auto unit = [&](f32x16& s, f32x16& dp, uint32_t at, int kbase, f32x16& sn, f32x16& dpn, uint32_t an) __attribute__((always_inline)) {
+        constexpr int EP = 16 / (2 * KS);
+        U4 kf[2], vf[2], p0, p1, x[2][2];
+        if (kbase + 32 > nkeys) {                     // keys past the end repeat one: their dS is dropped
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (kbase + 8 * (r >> 2) + 4 * hf + (r & 3) >= nkeys) dp[r] = 0.f;
+        }
+        const auto prob = [&](int r) __attribute__((always_inline)) { dp[r] *= __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], mul, nl)); };
+        kf[0].u = lds_read16(off[0] + an);
+        vf[0].u = lds_read16(off[0] + an + KV);
+        F3D_SB();
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            kf[ks].u = lds_read16(sK + at + off[ks]);
-            vf[ks].u = lds_read16(sV + at + off[ks]);
-        }
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            s[t] = f32x16{0};
-            dp[t] = f32x16{0};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s[t] = mfma(kf[ks], qf[t][ks], s[t]);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) dp[t] = mfma(vf[ks], gf[t][ks], dp[t]);
-        }
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) dp[t][r] = (dp[t][r] - dsum[t]) * __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], mul, nl[t]));
-            if (kbase + 32 > nkeys) {                 // keys past the end repeat one: their dS is dropped
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (kbase + 8 * (r >> 2) + 4 * hf + (r & 3) >= nkeys) dp[t][r] = 0.f;
+            if (ks + 1 < KS) {
+                kf[(ks + 1) & 1].u = lds_read16(off[ks + 1] + an);
+                vf[(ks + 1) & 1].u = lds_read16(off[ks + 1] + an + KV);
             }
+            if (ks == KS - 1) read_transposed<D>(x[0][0], x[0][1], toff + at, (toff + at) ^ T::FLIP, 0);
+            F3D_SB();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                (&p0[t].u.x)[e] = pack_bf16(dp[t][2 * e], dp[t][2 * e + 1]);
-                (&p1[t].u.x)[e] = pack_bf16(dp[t][8 + 2 * e], dp[t][8 + 2 * e + 1]);
-            }
+            for (int e = 0; e < EP; ++e) prob(2 * ks * EP + e);
+            F3D_SB();
+            sn = mfma(kf[ks & 1], qf[ks], ks == 0 ? f32x16{0} : sn);
+            F3D_SB();
+#pragma unroll
+            for (int e = 0; e < EP; ++e) prob((2 * ks + 1) * EP + e);
+            F3D_SB();
+            dpn = mfma(vf[ks & 1], gf[ks], ks == 0 ? minus_d : dpn);
+            F3D_SB();
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) (&p0.u.x)[e] = pack_bf16(dp[2 * e], dp[2 * e + 1]);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            U4 k0, k1;
-            read_transposed<D>(k0, k1, toff + at, (toff + at) ^ T::FLIP, mt);
+            if (mt + 1 < MT) read_transposed<D>(x[(mt + 1) & 1][0], x[(mt + 1) & 1][1], toff + at, (toff + at) ^ T::FLIP, mt + 1);
+            F3D_SB();
+            acc[mt] = mfma(x[mt & 1][0], p0, acc[mt]);
+            F3D_SB();
+            if (mt == 0) {
 #pragma unroll
-            for (int t = 0; t < QT; ++t) {
-                acc[t][mt] = mfma(k0, p0[t], acc[t][mt]);
-                acc[t][mt] = mfma(k1, p1[t], acc[t][mt]);
+                for (int e = 0; e < 4; ++e) (&p1.u.x)[e] = pack_bf16(dp[8 + 2 * e], dp[8 + 2 * e + 1]);
+                F3D_SB();
             }
+            acc[mt] = mfma(x[mt & 1][1], p1, acc[mt]);
+            F3D_SB();
         }
     };
-    for (int st = 0; st < nst; ++st) {
-        __builtin_amdgcn_s_waitcnt(vm_wait(0));       // this wave's loads of the stage are here
-        __syncthreads();                              // every wave's are, and the other buffer has been read
-        if (st + 1 < nst) dma_stage(st + 1);
-        if (!busy) continue;
-        const uint32_t at = (st % NBUF) * S::BYTES;
-#pragma unroll 1
-        for (int t4 = 0; t4 < S::TILES && st * S::ROWS + t4 * 32 < nkeys; ++t4) tile(at + t4 * T::BYTES, st * S::ROWS + t4 * 32);
-    }
+
+    f32x16 sa, sb, da, db;
+    int buf = 0;
+    // A block's rows are asked for a block ahead, where the registers allow it
+    constexpr bool AHEAD = D <= 64;
+    U4 nq[KS], ng[KS], no[KS];
+    float nlse = 0.f;
+    uint32_t place = 0;
+    auto fetch_row = [&](int blk) __attribute__((always_inline)) {
+        const int r = min(first_row + blk * BM + wave * 32 + l32, max(live, 1) - 1);   // past the end, or behind the segment's length: a row that counts, dropped
+        const int i = divide(r, a.G, a.by_g), g = r - i * a.G;
+        place = (uint32_t)(qs.from + i) * (uint32_t)a.H + (uint32_t)(kh * a.G + g);
+        const uint64_t from = (uint64_t)place * T::ROWB + hf * 16;
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        if (row[t] < 0) continue;
-        float* const p = SPLIT ? b.part_dq + ((size_t)part * a.n_q * a.H + at_q[t]) * D : nullptr;
-        store_row<D, MT>(p, b.dq + at_q[t] * D, acc[t], hf, b.scale, takes[t] && nkeys > 0);
+        for (int ks = 0; ks < KS; ++ks) {
+            nq[ks].u = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.q) + from + ks * 32);
+            ng[ks].u = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(b.dout) + from + ks * 32);
+            no[ks].u = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.out) + from + ks * 32);
+        }
+        nlse = a.lse[place];
+    };
+    if (AHEAD) fetch_row(0);
+    for (int blk = 0; blk < blocks; ++blk) {
+        const int row = first_row + blk * BM + wave * 32 + l32;
+        const bool takes = row < live, busy = first_row + blk * BM + wave * 32 < live;
+        if (!AHEAD) fetch_row(blk);
+        {
+            float dot = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                qf[ks] = nq[ks];
+                gf[ks] = ng[ks];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t y = (&no[ks].u.x)[e], z = (&ng[ks].u.x)[e];
+                    dot += __uint_as_float(y << 16) * __uint_as_float(z << 16);
+                    dot += __uint_as_float(y & 0xFFFF0000u) * __uint_as_float(z & 0xFFFF0000u);
+                }
+            }
+            dot += __shfl_xor(dot, 32, 64);
+            if (takes && part == 0 && hf == 0) b.dsum[place] = dot;
+            nl = takes && nkeys > 0 ? -LOG2E * nlse : -1e30f;   // rows that take no part: probabilities exactly zero
+            if (AHEAD && blk + 1 < blocks) fetch_row(blk + 1);
+#pragma unroll
+            for (int r2 = 0; r2 < 16; ++r2) minus_d[r2] = -dot;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16{0};
+        }
+        if (stays) buf = 0;
+        if (nst > 0 && busy) {
+            sa = f32x16{0};
+            da = minus_d;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                U4 kf, vf;
+                kf.u = lds_read16(off[ks] + buf * S::BYTES);
+                vf.u = lds_read16(off[ks] + buf * S::BYTES + KV);
+                sa = mfma(kf, qf[ks], sa);
+                da = mfma(vf, gf[ks], da);
+            }
+        }
+        for (int st = 0; st < nst; ++st) {
+            const int bufn = buf + 1 == NBUF ? 0 : buf + 1;
+            const uint32_t at0 = buf * S::BYTES, an0 = bufn * S::BYTES;
+#pragma unroll
+            for (int t4 = 0; t4 < S::TILES; ++t4) {
+                if (t4 + 1 == S::TILES && !stays) {   // the hand-over of the forward kernel
+                    __builtin_amdgcn_s_waitcnt(vm_wait(0));
+                    __syncthreads();
+                    if (asked < total) request_next(bufn + 1 == NBUF ? 0 : bufn + 1);
+                }
+                const int kbase = st * S::ROWS + t4 * 32;
+                if (!busy || kbase >= nkeys) continue;
+                const uint32_t at = at0 + t4 * T::BYTES, an = t4 + 1 < S::TILES ? at + T::BYTES : an0;
+                if ((t4 & 1) == 0) unit(sa, da, at, kbase, sb, db, an);
+                else unit(sb, db, at, kbase, sa, da, an);
+            }
+            buf = bufn;
+        }
+        if (row >= rows) continue;
+        const int i = divide(row, a.G, a.by_g), g = row - i * a.G;
+        const size_t at = (size_t)(qs.from + i) * a.H + kh * a.G + g;
+        float* const p = SPLIT ? b.part_dq + ((size_t)part * a.n_q * a.H + at) * D : nullptr;
+        store_row<D, MT>(p, b.dq + at * D, acc, hf, b.scale, takes && nkeys > 0);
     }
 }
 
@@ -441,23 +488,30 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossB
     store_row<D, MT>(SPLIT ? p + b.row_parts * all : nullptr, b.dv + at, dv, hf, 1.0f, has);
 }
 
-// The parts of a gradient, four channels a thread; rows that no segment owns get zeros. y: a second gradient, whose parts follow
+// The parts of a gradient: GROUPS threads to four channels, each adds up every GROUPS-th part; rows that no segment owns get zeros. y: a
+// second gradient, whose parts follow. Many parts are few rows: one thread to all of 192 parts took 17 us for 77 states of 64 channels,
+// 16 of them take 5; three parts of 36 MB take 20 us with one and 76 with 16, most of which have none.
+template <int GROUPS>
 __global__ __launch_bounds__(256) void k_cross_bwd_join(const float* part, int parts, long long n, int row_pieces, const int32_t* offsets,
                                                         int segments, int n_rows, uint16_t* x, uint16_t* y)
 {
-    long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    constexpr int PIECES = 256 / GROUPS;
+    __shared__ float4 meet[GROUPS][PIECES + 1];
+    const int c = threadIdx.x % PIECES, k = threadIdx.x / PIECES;
+    long long i = (long long)blockIdx.x * PIECES + c;
     uint16_t* to = x;
-    if (i >= n) {
-        if (!y || i >= 2 * n) return;
+    const bool second = i >= n;
+    if (second) {
         i -= n;
         to = y;
         part += (size_t)parts * n * 4;
     }
+    const bool has = i < n && (!second || y);
     const long long row = i / row_pieces;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (row >= offset_of(offsets, n_rows, 0) && row < offset_of(offsets, n_rows, segments)) {
+    if (has && row >= offset_of(offsets, n_rows, 0) && row < offset_of(offsets, n_rows, segments)) {
 #pragma unroll 4
-        for (int p = 0; p < parts; ++p) {
+        for (int p = k; p < parts; p += GROUPS) {
             const float4 f = reinterpret_cast<const float4*>(part)[p * n + i];
             s.x += f.x;
             s.y += f.y;
@@ -465,7 +519,27 @@ __global__ __launch_bounds__(256) void k_cross_bwd_join(const float* part, int p
             s.w += f.w;
         }
     }
+    if (GROUPS > 1) {
+        meet[k][c] = s;
+        __syncthreads();
+        for (int g = 1; k == 0 && g < GROUPS; ++g) {
+            const float4 f = meet[g][c];
+            s.x += f.x;
+            s.y += f.y;
+            s.z += f.z;
+            s.w += f.w;
+        }
+    }
+    if (k != 0 || !has) return;
     reinterpret_cast<uint2*>(to)[i] = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
+}
+
+hipError_t join(const float* part, int parts, long long n, long long all, int row_pieces, const int32_t* offsets, int segments, int n_rows,
+                uint16_t* x, uint16_t* y, hipStream_t stream)
+{
+    if (parts >= 16) k_cross_bwd_join<16><<<(unsigned)((all + 15) / 16), 256, 0, stream>>>(part, parts, n, row_pieces, offsets, segments, n_rows, x, y);
+    else k_cross_bwd_join<1><<<(unsigned)((all + 255) / 256), 256, 0, stream>>>(part, parts, n, row_pieces, offsets, segments, n_rows, x, y);
+    return hipGetLastError();
 }
 
 template <int D>
@@ -475,17 +549,14 @@ hipError_t launch(const CrossBwdArgs& b, hipStream_t stream)
     hipError_t e;
     if (a.n_q > 0) {
         const unsigned grid = cross_grid((long long)a.slots * a.parts, a.K, a.turn);
-        constexpr int QT2 = D <= 32 ? 2 : 1;
-        if (a.parts > 1) k_cross_bwd_dq<D, 1, true><<<grid, 256, 0, stream>>>(b);
-        else if (a.row_tiles == 2) k_cross_bwd_dq<D, QT2, false><<<grid, 256, 0, stream>>>(b);
-        else k_cross_bwd_dq<D, 1, false><<<grid, 256, 0, stream>>>(b);
+        constexpr int THREADS = 64 * RowStage<D>::WAVES;
+        if (a.parts > 1) k_cross_bwd_dq<D, true><<<grid, THREADS, 0, stream>>>(b);
+        else k_cross_bwd_dq<D, false><<<grid, THREADS, 0, stream>>>(b);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (a.parts > 1) {
             const long long n = (long long)a.n_q * a.H * (D / 4);
-            k_cross_bwd_join<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(b.part_dq, a.parts, n, a.H * (D / 4), a.q_offsets, a.segments, a.n_q,
-                                                                           b.dq, nullptr);
-            e = hipGetLastError();
+            e = join(b.part_dq, a.parts, n, n, a.H * (D / 4), a.q_offsets, a.segments, a.n_q, b.dq, nullptr, stream);
             if (e != hipSuccess) return e;
         }
     }
@@ -497,9 +568,7 @@ hipError_t launch(const CrossBwdArgs& b, hipStream_t stream)
         if (e != hipSuccess) return e;
         if (b.row_parts > 1) {
             const long long n = (long long)a.n_kv * a.K * (D / 4);
-            k_cross_bwd_join<<<(unsigned)((2 * n + 255) / 256), 256, 0, stream>>>(b.part_dkv, b.row_parts, n, a.K * (D / 4), a.kv_offsets,
-                                                                               a.segments, a.n_kv, b.dk, b.dv);
-            e = hipGetLastError();
+            e = join(b.part_dkv, b.row_parts, n, 2 * n, a.K * (D / 4), a.kv_offsets, a.segments, a.n_kv, b.dk, b.dv, stream);
             if (e != hipSuccess) return e;
         }
     }

@@ -134,6 +134,19 @@ __device__ __forceinline__ void read_transposed(U4& x0, U4& x1, uint32_t at, uin
     x1.u = make_uint4(y2.x, y2.y, y3.x, y3.y);
 }
 
+// Keys and values in LDS for the kernels whose waves own query rows: stages of ROWS keys, NBUF of them resident.
+template <int D>
+struct RowStage {
+    using T = Tile<D>;
+    static constexpr int WAVES = D == 128 ? 8 : 4;    // 128: three stages leave room for one workgroup on a compute unit
+    static constexpr int ROWS = D == 16 ? 128 : 64;
+    static constexpr int TILES = ROWS / 32;
+    static constexpr int BYTES = ROWS * T::ROWB;      // of K, and of V
+    static constexpr int NBUF = D == 32 ? 4 : 3;
+    static constexpr int LPW = ROWS * T::NC / (64 * WAVES);
+    static constexpr int TOTAL = NBUF * 2 * BYTES;
+};
+
 constexpr int vm_wait(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }   // s_waitcnt operand: the memory counter alone
 
 }  // namespace

@@ -693,7 +693,6 @@ static int fill_cross_args(f3d::CrossArgs& a, const CrossSizes& s, const f3d::Cr
     if (f16) a.s_mul = fminf(a.s_mul, 0x1p90f);   // as in f3d_bucket_swin_attn_f16
     a.f16 = f16;
     a.few = p.few;
-    a.row_tiles = p.row_tiles;
     a.run_shift = p.run_shift;
     a.slots = p.slots;
     a.parts = p.parts;
