@@ -47,6 +47,7 @@ struct CrossBwdArgs {
     uint16_t* dv;
     float scale;
     float* part_dq;             // [parts][n_q * H][head_dim], where parts > 1
+    int short_tiles;            // 0: the two kernels; else one, for segments of up to 32 short_tiles keys
     int kv_turn;
     int kv_slots;               // blocks of 128 keys over all segments
     int row_parts;              // parts the query rows of a segment are split into
@@ -57,11 +58,12 @@ struct CrossBwdArgs {
 // What a call takes: a rule on sizes the host knows
 struct CrossPlan {
     int few, run_shift, slots, parts, chunk;
-    int kv_slots, row_parts, row_chunk;   // backward
+    int short_tiles, kv_slots, row_parts, row_chunk;   // backward
 };
 CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_q, long long max_kv, int heads, int kv_heads, int head_dim, bool backward);
 
 hipError_t cross_launch(const CrossArgs& a, int head_dim, hipStream_t stream);
+hipError_t cross_bwd_short_launch(const CrossBwdArgs& a, int head_dim, int tiles, hipStream_t stream);
 hipError_t cross_bwd_launch(const CrossBwdArgs& a, int head_dim, hipStream_t stream);
 
 }  // namespace f3d

@@ -589,6 +589,18 @@ CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_
         while (p.run_shift < block_shift + 3 && (blocks >> (p.run_shift - block_shift + 1)) >= 12 * CUS) ++p.run_shift;
     p.slots = (int)((rows >> p.run_shift) + segments);
     if (!backward) return p;
+    if (((head_dim == 16 && max_kv <= 128) || (head_dim == 32 && max_kv <= 96)) && n_q > 0 && n_kv > 0) {   // every key's gradients in registers: one kernel
+        p.short_tiles = (int)((max_kv + 31) / 32);
+        p.parts = 1;
+        p.kv_slots = segments;
+        // two workgroups per compute unit; 256 rows each, two tiles a wave, at least
+        const long long all = (long long)segments * kv_heads, most = (max_q * group + 255) / 256;
+        long long row_parts = (2 * CUS + all - 1) / all;
+        if (row_parts > most) row_parts = most;
+        p.row_chunk = (int)(((max_q * group + row_parts - 1) / row_parts + 127) / 128 * 128);
+        p.row_parts = (int)((max_q * group + p.row_chunk - 1) / p.row_chunk);
+        return p;
+    }
     p.kv_slots = (int)(n_kv / 128 + segments);
     const long long kv_work = n_kv / 128 > segments ? n_kv / 128 : segments;
     long long row_parts = 1;

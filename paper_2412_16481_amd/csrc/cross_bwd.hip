@@ -45,19 +45,6 @@ __device__ __forceinline__ void store_row(float* part, uint16_t* to, const f32x1
     }
 }
 
-// Rows of a tensor that no segment owns get zeros from all workgroups of a launch together; there are none as a rule
-__device__ __forceinline__ void zero_rest(const int32_t* offsets, int segments, int n, uint32_t row_bytes, uint16_t* x, uint16_t* y)
-{
-    const int before = offset_of(offsets, n, 0), from = offset_of(offsets, n, segments);
-    if (before == 0 && from == n) return;
-    const long long head = (long long)min(before, from) * row_bytes / 16, tail = (long long)from * row_bytes / 16, all = (long long)n * row_bytes / 16;
-    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < head + all - tail; i += (long long)gridDim.x * blockDim.x) {
-        const long long at = i < head ? i : tail + (i - head);
-        reinterpret_cast<uint4*>(x)[at] = make_uint4(0, 0, 0, 0);
-        if (y) reinterpret_cast<uint4*>(y)[at] = make_uint4(0, 0, 0, 0);
-    }
-}
-
 // Runs of row blocks, stages and their hand-over as in the forward kernel. Per tile of 32 keys a wave has 2 KS MFMAs for the scores and dP
 // (of the NEXT tile, issued between the exponentials of the current one; -D is the accumulator dP starts from) and 2 MT for dQ.
 template <int D, bool SPLIT>
@@ -73,7 +60,7 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross_bwd_dq(Cro
     constexpr uint32_t KV = NBUF * S::BYTES;          // from a row of K to the same of V
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    if (!SPLIT) zero_rest(a.q_offsets, a.segments, a.n_q, (uint32_t)a.H * T::ROWB, b.dq, nullptr);
+    if (!SPLIT) zero_rows(b.dq, a.n_q, offset_of(a.q_offsets, a.n_q, 0), offset_of(a.q_offsets, a.n_q, a.segments), (uint32_t)a.H * T::ROWB);
     const uint32_t u = piece_of(a.turn);
     const uint32_t x = u / (uint32_t)a.K;
     const int kh = (int)(u - x * a.K), slot = (int)(SPLIT ? x / (uint32_t)a.parts : x), part = SPLIT ? (int)(x - (uint32_t)slot * a.parts) : 0;
@@ -296,7 +283,11 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossB
     const uint32_t sQ = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sG = sQ + NBUF * S::BYTES;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    if (!SPLIT) zero_rest(a.kv_offsets, a.segments, a.n_kv, (uint32_t)a.K * T::ROWB, b.dk, b.dv);
+    if (!SPLIT) {
+        const int from = offset_of(a.kv_offsets, a.n_kv, 0), to = offset_of(a.kv_offsets, a.n_kv, a.segments);
+        zero_rows(b.dk, a.n_kv, from, to, (uint32_t)a.K * T::ROWB);
+        zero_rows(b.dv, a.n_kv, from, to, (uint32_t)a.K * T::ROWB);
+    }
     const uint32_t u = piece_of(b.kv_turn);
     const uint32_t x = u / (uint32_t)a.K;
     const int kh = (int)(u - x * a.K), slot = (int)(SPLIT ? x / (uint32_t)b.row_parts : x), part = SPLIT ? (int)(x - (uint32_t)slot * b.row_parts) : 0;
@@ -547,6 +538,12 @@ hipError_t launch(const CrossBwdArgs& b, hipStream_t stream)
 {
     const CrossArgs& a = b.f;
     hipError_t e;
+    if (b.short_tiles > 0) {                          // one kernel for everything but the join
+        e = cross_bwd_short_launch(b, D, b.short_tiles, stream);
+        if (e != hipSuccess || b.row_parts == 1) return e;
+        const long long n = (long long)a.n_kv * a.K * (D / 4);
+        return join(b.part_dkv, b.row_parts, n, 2 * n, a.K * (D / 4), a.kv_offsets, a.segments, a.n_kv, b.dk, b.dv, stream);
+    }
     if (a.n_q > 0) {
         const unsigned grid = cross_grid((long long)a.slots * a.parts, a.K, a.turn);
         constexpr int THREADS = 64 * RowStage<D>::WAVES;

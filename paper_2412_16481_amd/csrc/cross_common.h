@@ -134,6 +134,16 @@ __device__ __forceinline__ void read_transposed(U4& x0, U4& x1, uint32_t at, uin
     x1.u = make_uint4(y2.x, y2.y, y3.x, y3.y);
 }
 
+// Rows [0, from) and [to, n) of a tensor, which no segment owns, get zeros from all workgroups of the grid's first dimension together; there
+// are none as a rule
+__device__ __forceinline__ void zero_rows(uint16_t* x, int n, int from, int to, uint32_t row_bytes)
+{
+    if (from == 0 && to == n) return;
+    const long long head = (long long)min(from, to) * row_bytes / 16, tail = (long long)to * row_bytes / 16, all = (long long)n * row_bytes / 16;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < head + all - tail; i += (long long)gridDim.x * blockDim.x)
+        reinterpret_cast<uint4*>(x)[i < head ? i : tail + (i - head)] = make_uint4(0, 0, 0, 0);
+}
+
 // Keys and values in LDS for the kernels whose waves own query rows: stages of ROWS keys, NBUF of them resident.
 template <int D>
 struct RowStage {

@@ -814,6 +814,7 @@ int f3d_cross_attn_bwd(const void* q, const void* k, const void* v, const void* 
     b.dv = (uint16_t*)dv;
     b.part_dq = (float*)((char*)workspace + dsum);
     b.part_dkv = (float*)((char*)workspace + dsum + part);
+    b.short_tiles = p.short_tiles;
     b.kv_slots = p.kv_slots;
     b.kv_turn = f3d::cross_turn((long long)p.kv_slots * p.row_parts, b.f.K);
     b.row_parts = p.row_parts;
