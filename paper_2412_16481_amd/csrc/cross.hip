@@ -292,20 +292,21 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
 template <int D>
 struct FewStage {
     using T = Tile<D>;
-    static constexpr int ROWS = 128;
+    static constexpr int WAVES = D == 128 ? 2 : 4;    // 128: two workgroups on a compute unit
+    static constexpr int ROWS = 32 * WAVES;
     static constexpr int BYTES = ROWS * T::ROWB;      // of K, and of V
     static constexpr int NBUF = D >= 64 ? 2 : 3;
-    static constexpr int LPW = ROWS * T::NC / 256;    // loads per lane, stage and tensor
+    static constexpr int LPW = ROWS * T::NC / (64 * WAVES);    // loads per lane, stage and tensor
     static constexpr int TOTAL = NBUF * 2 * BYTES;
 };
 
 template <int D, bool F16, bool SPLIT>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a)
+__global__ __launch_bounds__(64 * FewStage<D>::WAVES, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a)
 {
     using T = Tile<D>;
     using S = FewStage<D>;
     using E = Half<F16>;
-    constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF;
+    constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF, NW = S::WAVES;
     constexpr int BM = 32, SHIFT = 5;                 // rows of a workgroup
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::TOTAL];
     const uint32_t sK = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sV = sK + NBUF * S::BYTES;
@@ -435,11 +436,11 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a
         lr = __int_as_float(su[0]) + __int_as_float(su[1]);
     }
 
-    // ---- the four waves' results meet in LDS: row by row, channels in order
+    // ---- the waves' results meet in LDS: row by row, channels in order
     constexpr int P = D + 4;                      // floats from one row to the next
-    static_assert(4 * 32 * P * 4 <= S::TOTAL, "room for the results");
+    static_assert(NW * 32 * P * 4 <= S::TOTAL, "room for the results");
     float* const meet = reinterpret_cast<float*>(smem);
-    __shared__ float sm_[4][32], sl_[4][32], sr_[4][32];
+    __shared__ float sm_[NW][32], sl_[NW][32], sr_[NW][32];
     __syncthreads();                              // the last stage has been read
     if (hf == 0) {
         sm_[wave][l32] = m;
@@ -454,17 +455,19 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a
                 make_float4(o[mt][4 * r4], o[mt][4 * r4 + 1], o[mt][4 * r4 + 2], o[mt][4 * r4 + 3]);
     }
     __syncthreads();
-    constexpr int EACH = D / 8;                   // channels of a thread: eight of them to a row
-    const int rr = tid >> 3, c0 = (tid & 7) * EACH;
+    constexpr int TPR = 2 * NW, EACH = D / TPR;       // threads of a row, channels of a thread
+    const int rr = tid / TPR, c0 = (tid % TPR) * EACH;
     const long long r = blk * BM + rr;
     if (r >= rows) return;
     const int i = divide((int)r, a.G, a.by_g), g = (int)r - i * a.G;
     const size_t at = (size_t)(qs.from + i) * a.H + kh * a.G + g;
     const bool counts = r < live;
-    const float top = fmaxf(fmaxf(sm_[0][rr], sm_[1][rr]), fmaxf(sm_[2][rr], sm_[3][rr]));
-    float w[4], sum = 0.f, rounded = 0.f;
+    float top = sm_[0][rr];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {                 // a wave without keys has -inf, and so has `top` where all have
+    for (int k = 1; k < NW; ++k) top = fmaxf(top, sm_[k][rr]);
+    float w[NW], sum = 0.f, rounded = 0.f;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {                // a wave without keys has -inf, and so has `top` where all have
         w[k] = sm_[k][rr] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm_[k][rr] - top);
         sum += w[k] * sl_[k][rr];
         rounded += w[k] * sr_[k][rr];
@@ -474,14 +477,14 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a
     for (int c = 0; c < EACH; ++c) {
         y[c] = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < NW; ++k)
             if (w[k] != 0.f) y[c] += w[k] * meet[(k * 32 + rr) * P + c0 + c];
     }
     if (!counts) sum = 0.f;
     if (SPLIT) {
         const size_t pa = (size_t)part * a.n_q * a.H + at;
-        if ((tid & 7) == 0) a.part_ml[pa] = make_float2(sum > 0.f ? top : -INFINITY, rounded);
-        if (a.lse && (tid & 7) == 0) a.part_l[pa] = sum;
+        if (tid % TPR == 0) a.part_ml[pa] = make_float2(sum > 0.f ? top : -INFINITY, rounded);
+        if (a.lse && tid % TPR == 0) a.part_l[pa] = sum;
         if (sum > 0.f) {
 #pragma unroll
             for (int c = 0; c < EACH; c += 2) *reinterpret_cast<float2*>(a.part_o + pa * D + c0 + c) = make_float2(y[c], y[c + 1]);
@@ -489,7 +492,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_few(CrossArgs a
         return;
     }
     const float inv = sum > 0.f ? 1.0f / rounded : 0.f;
-    if (a.lse && (tid & 7) == 0) a.lse[at] = sum > 0.f ? (top + __log2f(sum)) * LN2 : -INFINITY;
+    if (a.lse && tid % TPR == 0) a.lse[at] = sum > 0.f ? (top + __log2f(sum)) * LN2 : -INFINITY;
 #pragma unroll
     for (int c = 0; c < EACH; c += 2) {
         const uint32_t pair = sum > 0.f ? E::pack(y[c] * inv, y[c + 1] * inv) : 0u;
@@ -533,11 +536,11 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a)
 template <int D, bool F16>
 hipError_t launch(const CrossArgs& a, hipStream_t stream)
 {
-    const unsigned grid = cross_grid((long long)a.slots * a.parts, a.K, a.turn), threads = 64 * RowStage<D>::WAVES;
+    const unsigned grid = cross_grid((long long)a.slots * a.parts, a.K, a.turn), threads = 64 * RowStage<D>::WAVES, few_threads = 64 * FewStage<D>::WAVES;
     const bool split = a.parts > 1;
     if (a.few) {
-        if (split) k_cross_few<D, F16, true><<<grid, 256, 0, stream>>>(a);
-        else k_cross_few<D, F16, false><<<grid, 256, 0, stream>>>(a);
+        if (split) k_cross_few<D, F16, true><<<grid, few_threads, 0, stream>>>(a);
+        else k_cross_few<D, F16, false><<<grid, few_threads, 0, stream>>>(a);
     } else if (split) {
         if (a.lse) k_cross<D, F16, true, true><<<grid, threads, 0, stream>>>(a);
         else k_cross<D, F16, true, false><<<grid, threads, 0, stream>>>(a);

@@ -290,8 +290,8 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossB
     }
     const uint32_t u = piece_of(b.kv_turn);
     const uint32_t x = u / (uint32_t)a.K;
-    const int kh = (int)(u - x * a.K), slot = (int)(SPLIT ? x / (uint32_t)b.row_parts : x), part = SPLIT ? (int)(x - (uint32_t)slot * b.row_parts) : 0;
-    if (slot >= b.kv_slots) return;
+    const int kh = (int)(u - x * a.K), part = SPLIT ? (int)(x / (uint32_t)b.kv_slots) : 0, slot = (int)(x - (uint32_t)part * b.kv_slots);
+    if (SPLIT ? part >= b.row_parts : slot >= b.kv_slots) return;
     const int seg = segment_of(a.kv_offsets, a.n_kv, a.segments, 1, SHIFT, slot);
     const Rows qs = rows_of(a.q_offsets, a.q_lens, a.n_q, seg), kv = rows_of(a.kv_offsets, a.kv_lens, a.n_kv, seg);
     const long long blk = slot - first_slot(a.kv_offsets, a.n_kv, seg, 1, SHIFT);
@@ -479,6 +479,186 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossB
     store_row<D, MT>(SPLIT ? p + b.row_parts * all : nullptr, b.dv + at, dv, hf, 1.0f, has);
 }
 
+// The same for 128 channels, where one wave's gradients of 32 keys take 128 registers. Eight waves, two to a SIMD: four tiles of keys by
+// two tiles of rows of a stage, so that one wave's products run beside another's exponentials; V stays in LDS, what would be its registers
+// make room for that. The two waves of a key tile add up at the end.
+template <bool SPLIT>
+__global__ __launch_bounds__(512, 2) void k_cross_bwd_dkdv_wide(CrossBwdArgs b)
+{
+    constexpr int D = 128, ROWS = 64, NBUF = 3, BM = 128, SHIFT = 7;
+    using T = Tile<D>;
+    constexpr int KS = T::KS, MT = T::MT, BYTES = ROWS * T::ROWB, LPW = ROWS * T::NC / 512, VBYTES = BM * T::ROWB;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[VBYTES + NBUF * 2 * BYTES];
+    __shared__ __attribute__((aligned(16))) float sl[NBUF][ROWS], sd[NBUF][ROWS];
+    const CrossArgs& a = b.f;
+    const uint32_t sV = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sQ = sV + VBYTES;
+    constexpr uint32_t GQ = NBUF * BYTES;             // from a row of Q to the same of dO
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kt = wave & 3, group = wave >> 2;
+    if (!SPLIT) {
+        const int from = offset_of(a.kv_offsets, a.n_kv, 0), to = offset_of(a.kv_offsets, a.n_kv, a.segments);
+        zero_rows(b.dk, a.n_kv, from, to, (uint32_t)a.K * T::ROWB);
+        zero_rows(b.dv, a.n_kv, from, to, (uint32_t)a.K * T::ROWB);
+    }
+    const uint32_t u = piece_of(b.kv_turn);
+    const uint32_t x = u / (uint32_t)a.K;
+    const int kh = (int)(u - x * a.K), part = SPLIT ? (int)(x / (uint32_t)b.kv_slots) : 0, slot = (int)(x - (uint32_t)part * b.kv_slots);
+    if (SPLIT ? part >= b.row_parts : slot >= b.kv_slots) return;
+    const int seg = segment_of(a.kv_offsets, a.n_kv, a.segments, 1, SHIFT, slot);
+    const Rows qs = rows_of(a.q_offsets, a.q_lens, a.n_q, seg), kv = rows_of(a.kv_offsets, a.kv_lens, a.n_kv, seg);
+    const long long blk = slot - first_slot(a.kv_offsets, a.n_kv, seg, 1, SHIFT);
+    if (blk < 0 || blk * BM >= kv.span) return;
+    const int row0 = SPLIT ? part * b.row_chunk : 0, live = qs.len * a.G;
+    const int nrows = blk * BM >= kv.len ? 0 : SPLIT ? min(max(live - row0, 0), b.row_chunk) : live;
+
+    const uint32_t row_bytes = (uint32_t)a.H * T::ROWB;
+    const float mul = a.s_mul, lmul = -LOG2E / a.s_mul;
+    int srow[LPW];
+    uint32_t scol[LPW];
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+        const int p = (wave * LPW + i) * 64 + lane;
+        srow[i] = p / T::NC;
+        scol[i] = ((p % T::NC) ^ T::swizzle(srow[i])) << 4;
+    }
+    float nl = 0.f, nd = 0.f;                         // of row `tid` of the stage requested last
+    auto request = [&](int st) __attribute__((always_inline)) {
+        const uint32_t to = (st % NBUF) * BYTES;
+        if (tid < ROWS) {
+            const int r = st * ROWS + tid, rc = row0 + min(r, nrows - 1);
+            const int q = divide(rc, a.G, a.by_g), g = rc - q * a.G;
+            const size_t at = (size_t)(qs.from + q) * a.H + kh * a.G + g;
+            const float l = a.lse[at], d = b.dsum[at];
+            nl = r < nrows ? l * lmul : -1e30f;
+            nd = -d;
+        }
+#pragma unroll
+        for (int i = 0; i < LPW; ++i) {
+            const int r = row0 + min(st * ROWS + srow[i], nrows - 1);
+            const int q = divide(r, a.G, a.by_g), g = r - q * a.G;
+            const uint64_t at = (uint64_t)(qs.from + q) * row_bytes + (uint32_t)(kh * a.G + g) * T::ROWB + scol[i];
+            lds_dma16(reinterpret_cast<const char*>(a.q) + at, sQ + to + (wave * LPW + i) * 1024);
+            lds_dma16(reinterpret_cast<const char*>(b.dout) + at, sQ + GQ + to + (wave * LPW + i) * 1024);
+        }
+    };
+    auto keep_sums = [&](int st) __attribute__((always_inline)) {
+        if (tid < ROWS) {
+            sl[st % NBUF][tid] = nl;
+            sd[st % NBUF][tid] = nd;
+        }
+    };
+    const int nst = (nrows + ROWS - 1) / ROWS;
+    const long long key = blk * BM + kt * 32 + l32;
+    const bool busy = blk * BM + kt * 32 < kv.len;
+    U4 kf[KS];
+    f32x16 dk[MT], dv[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) dk[mt] = dv[mt] = f32x16{0};
+    if (nst > 0) {
+#pragma unroll
+        for (int i = 0; i < VBYTES / 8192; ++i) {     // V: rows past the end repeat the last one
+            const int p = (wave * (VBYTES / 8192) + i) * 64 + lane, r = p / T::NC;
+            const long long k = min(blk * BM + r, (long long)kv.len - 1);
+            const uint64_t at = ((uint64_t)(kv.from + k) * a.K + kh) * T::ROWB + (((p % T::NC) ^ T::swizzle(r & 31)) << 4);
+            lds_dma16(reinterpret_cast<const char*>(a.v) + at, sV + (wave * (VBYTES / 8192) + i) * 1024);
+        }
+        request(0);
+        keep_sums(0);
+        if (nst > 1) {
+            request(1);
+            keep_sums(1);
+        }
+        const size_t at = ((size_t)(kv.from + min(key, (long long)kv.len - 1)) * a.K + kh) * D + hf * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[ks].u = *reinterpret_cast<const uint4*>(a.k + at + ks * 16);
+    }
+    uint32_t off[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) off[ks] = T::row_piece(lane, ks);
+    const uint32_t tr = sQ + T::transposed(lane), sv = sV + kt * T::BYTES;
+
+    for (int st = 0; st < nst; ++st) {
+        // the stage is here once only what was asked for after it is outstanding
+        if (st > 0 && st + 1 < nst) __builtin_amdgcn_s_waitcnt(vm_wait(2 * LPW));
+        else __builtin_amdgcn_s_waitcnt(vm_wait(0));
+        __syncthreads();                              // every wave's part of it is, and stage st - 1 has been read
+        if (st + 2 < nst) request(st + 2);
+        if (busy) {
+            const int buf = st % NBUF;
+            const uint32_t at = buf * BYTES + group * T::BYTES;
+            f32x16 s, dp;
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                const float4 l = *reinterpret_cast<const float4*>(&sl[buf][group * 32 + 8 * r4 + 4 * hf]);
+                const float4 d = *reinterpret_cast<const float4*>(&sd[buf][group * 32 + 8 * r4 + 4 * hf]);
+                s[4 * r4] = l.x, s[4 * r4 + 1] = l.y, s[4 * r4 + 2] = l.z, s[4 * r4 + 3] = l.w;
+                dp[4 * r4] = d.x, dp[4 * r4 + 1] = d.y, dp[4 * r4 + 2] = d.z, dp[4 * r4 + 3] = d.w;
+            }
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                U4 qf, gf, vf;
+                qf.u = lds_read16(sQ + at + off[ks]);
+                gf.u = lds_read16(sQ + GQ + at + off[ks]);
+                vf.u = lds_read16(sv + off[ks]);
+                s = mfma(qf, kf[ks], s);
+                dp = mfma(gf, vf, dp);
+            }
+            U4 p0, p1, d0, d1;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[r] = __builtin_amdgcn_exp2f(s[r] * mul);
+                dp[r] *= s[r];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                (&p0.u.x)[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
+                (&p1.u.x)[e] = pack_bf16(s[8 + 2 * e], s[8 + 2 * e + 1]);
+                (&d0.u.x)[e] = pack_bf16(dp[2 * e], dp[2 * e + 1]);
+                (&d1.u.x)[e] = pack_bf16(dp[8 + 2 * e], dp[8 + 2 * e + 1]);
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                U4 g0, g1, q0, q1;
+                read_transposed<D>(g0, g1, tr + GQ + at, (tr + GQ + at) ^ T::FLIP, mt);
+                read_transposed<D>(q0, q1, tr + at, (tr + at) ^ T::FLIP, mt);
+                dv[mt] = mfma(g0, p0, dv[mt]);
+                dk[mt] = mfma(q0, d0, dk[mt]);
+                dv[mt] = mfma(g1, p1, dv[mt]);
+                dk[mt] = mfma(q1, d1, dk[mt]);
+            }
+        }
+        if (st + 2 < nst) keep_sums(st + 2);
+    }
+    // ---- the second wave of every key tile hands its sums over: dk, then dv, [4][4][16][64]
+    float* const meet = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        f32x16(&acc)[MT] = which ? dv : dk;
+        __syncthreads();
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                if (group == 1) meet[(kt * MT * 16 + mt * 16 + r) * 64 + lane] = acc[mt][r];
+            }
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[mt][r] += meet[(kt * MT * 16 + mt * 16 + r) * 64 + lane];
+            }
+        }
+    }
+    if (group == 1 || key >= kv.span) return;
+    const bool has = key < kv.len && nrows > 0;
+    const size_t at = ((size_t)(kv.from + key) * a.K + kh) * D, all = (size_t)a.n_kv * a.K * D;
+    float* const p = SPLIT ? b.part_dkv + part * all + at : nullptr;
+    store_row<D, MT>(p, b.dk + at, dk, hf, b.scale, has);
+    store_row<D, MT>(SPLIT ? p + b.row_parts * all : nullptr, b.dv + at, dv, hf, 1.0f, has);
+}
+
 // The parts of a gradient: GROUPS threads to four channels, each adds up every GROUPS-th part; rows that no segment owns get zeros. y: a
 // second gradient, whose parts follow. Many parts are few rows: one thread to all of 192 parts took 17 us for 77 states of 64 channels,
 // 16 of them take 5; three parts of 36 MB take 20 us with one and 76 with 16, most of which have none.
@@ -559,8 +739,13 @@ hipError_t launch(const CrossBwdArgs& b, hipStream_t stream)
     }
     if (a.n_kv > 0) {
         const unsigned grid = cross_grid((long long)b.kv_slots * b.row_parts, a.K, b.kv_turn);
-        if (b.row_parts > 1) k_cross_bwd_dkdv<D, true><<<grid, 256, 0, stream>>>(b);
-        else k_cross_bwd_dkdv<D, false><<<grid, 256, 0, stream>>>(b);
+        if constexpr (D == 128) {
+            if (b.row_parts > 1) k_cross_bwd_dkdv_wide<true><<<grid, 512, 0, stream>>>(b);
+            else k_cross_bwd_dkdv_wide<false><<<grid, 512, 0, stream>>>(b);
+        } else {
+            if (b.row_parts > 1) k_cross_bwd_dkdv<D, true><<<grid, 256, 0, stream>>>(b);
+            else k_cross_bwd_dkdv<D, false><<<grid, 256, 0, stream>>>(b);
+        }
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (b.row_parts > 1) {
