@@ -30,13 +30,13 @@ constexpr float LN2 = 0.6931471805599453f;
 
 // Many query rows: a wave owns a tile of 32 of them at a time.
 template <int D, bool F16, bool SPLIT, bool LSE>
-__global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs a)
+__global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a)
 {
     using T = Tile<D>;
     using S = RowStage<D>;
     using E = Half<F16>;
-    constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF, NW = S::WAVES;
-    constexpr int BM = 32 * NW;                  // rows of a workgroup at a time
+    constexpr int KS = T::KS, MT = T::MT, NBUF = S::NBUF;
+    constexpr int BM = 128;                           // rows of a workgroup at a time
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::TOTAL];
     const uint32_t sK = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem, sV = sK + NBUF * S::BYTES;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
@@ -57,41 +57,9 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
     const int key0 = SPLIT ? part * a.chunk : 0;
     const int nkeys = first_row >= live ? 0 : SPLIT ? min(max(kv.len - key0, 0), a.chunk) : kv.len;   // this workgroup's
 
-    // ---- staging
     const uint32_t row_bytes = (uint32_t)a.K * T::ROWB;
-    const uint64_t first = (uint64_t)(kv.from + key0) * row_bytes + (uint64_t)kh * T::ROWB;
-    int srow[LPW];
-    uint32_t scol[LPW];
-#pragma unroll
-    for (int i = 0; i < LPW; ++i) {
-        const int p = (wave * LPW + i) * 64 + lane;
-        srow[i] = p / T::NC;
-        scol[i] = ((p % T::NC) ^ T::swizzle(srow[i])) << 4;
-    }
-    auto request = [&](int st, int buf) __attribute__((always_inline)) {
-        const uint32_t to = buf * S::BYTES;
-#pragma unroll
-        for (int i = 0; i < LPW; ++i) {
-            const int key = min(st * S::ROWS + srow[i], nkeys - 1);   // past the end: the last key again, masked
-            const uint64_t at = first + (uint64_t)(uint32_t)key * row_bytes + scol[i];
-            lds_dma16(reinterpret_cast<const char*>(a.k) + at, sK + to + (wave * LPW + i) * 1024);
-            lds_dma16(reinterpret_cast<const char*>(a.v) + at, sV + to + (wave * LPW + i) * 1024);
-        }
-    };
-    const int nst = (nkeys + S::ROWS - 1) / S::ROWS;
-    const bool stays = nst <= NBUF;                   // all keys are resident: staged once, and no barrier behind the first
-    int total = stays ? nst : nst * blocks;           // stages to come, over all row blocks
-    int asked = 0, ask_st = 0;                        // stages requested, the next one's keys
-    auto request_next = [&](int buf) __attribute__((always_inline)) {
-        request(ask_st, buf);
-        ++asked;
-        ask_st = ask_st + 1 == nst ? 0 : ask_st + 1;
-    };
-    if (total > 0) request_next(0);
-    if (total > 1) request_next(1);
-#pragma unroll
-    for (int i = 2; i < NBUF; ++i)
-        if (stays && total > i) request_next(i);
+    KeyRing<D> ring;
+    ring.start(a.k, a.v, (uint64_t)(kv.from + key0) * row_bytes + (uint64_t)kh * T::ROWB, row_bytes, nkeys, blocks, sK, wave);
 
     uint32_t koff[KS];
 #pragma unroll
@@ -111,7 +79,7 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
         for (int ks = 0; ks < KS; ++ks) qf[ks].u = *reinterpret_cast<const uint4*>(from + ks * 32);
     };
     fetch_row(0);
-    if (total > 0) {
+    if (nkeys > 0) {
         __builtin_amdgcn_s_waitcnt(vm_wait(0));
         __syncthreads();                              // the stages asked for so far are here
     }
@@ -190,7 +158,7 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
         }
     };
 
-    int buf = 0;
+    int buf = 0, read = 0;                            // read: stages over all row blocks
     // One sweep over the keys for the block of rows in qf. The optimistic one takes the exponentials against the fixed reference 0: exact
     // as long as the sum stays well inside the range of the formats, which is looked at afterwards.
     auto sweep = [&](bool busy) __attribute__((always_inline)) {
@@ -198,31 +166,31 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
         l = lr = 0.f;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) o[mt] = f32x16{0};
-        if (stays) buf = 0;
+        if (ring.stays) buf = 0;
         read_k(kf, buf * S::BYTES);
         sa = f32x16{0};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) sa = E::mfma(kf[ks], qf[ks], sa);
-        for (int st = 0; st < nst; ++st) {
+        auto stage = [&](int st, auto first_tile) __attribute__((always_inline)) {
             const int bufn = buf + 1 == NBUF ? 0 : buf + 1;
             const uint32_t at0 = buf * S::BYTES, an0 = bufn * S::BYTES;
 #pragma unroll
             for (int t4 = 0; t4 < S::TILES; ++t4) {
-                if (t4 + 1 == S::TILES && !stays) {
-                    // The next stage is handed over to the readers, and the buffer of the one before this is asked for again: whoever
-                    // arrives has its own loads of the next stage and has read the last of the one before.
-                    __builtin_amdgcn_s_waitcnt(vm_wait(0));
-                    __syncthreads();
-                    if (asked < total) request_next(bufn + 1 == NBUF ? 0 : bufn + 1);
-                }
+                if (t4 + 1 == S::TILES && !ring.stays) ring.hand_over(buf, ++read);
                 const int kbase = st * S::ROWS + t4 * 32;
                 if (!busy || kbase >= nkeys) continue;
                 const uint32_t at = at0 + t4 * T::BYTES, an = t4 + 1 < S::TILES ? at + T::BYTES : an0;
                 read_k(kf, an);                       // what is computed ahead of the last tile is never used
-                if ((t4 & 1) == 0) unit(sa, at, kbase, sb);
+                if (((t4 + decltype(first_tile)::value) & 1) == 0) unit(sa, at, kbase, sb);
                 else unit(sb, at, kbase, sa);
             }
             buf = bufn;
+        };
+        for (int st = 0; st < ring.nst; st += S::LOOP) {
+            stage(st, std::integral_constant<int, 0>{});
+            if (S::LOOP == 1) continue;
+            if (st + 1 >= ring.nst) break;
+            stage(st + 1, std::integral_constant<int, 1>{});
         }
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(lr), __float_as_int(lr), false, false);
         lr = __int_as_float(sw[0]) + __int_as_float(sw[1]);
@@ -233,19 +201,18 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross(CrossArgs 
     for (int blk = 0; blk < blocks; ++blk) {
         const bool busy = first_row + blk * BM + wave * 32 < live;   // this wave has rows with results
         robust = false;
-        while (nst > 0) {
+        while (nkeys > 0) {
             sweep(busy);
             if (robust) break;
             const bool bad = row_of(blk) < live && !(lr > E::SUM_LO && lr < E::SUM_HI);
             // keys that stay: every wave for itself
-            robust = stays ? __builtin_amdgcn_ballot_w64(bad) != 0 : __syncthreads_or(bad) != 0;
+            robust = ring.stays ? __builtin_amdgcn_ballot_w64(bad) != 0 : __syncthreads_or(bad) != 0;
             if (!robust) break;
-            if (stays) continue;
+            if (ring.stays) continue;
             // the same keys once more: what is on its way for the next block are their first stages
-            total += nst;
+            ring.total += ring.nst;
             if (blk + 1 == blocks) {                  // nothing is: all stages asked for have been read
-                request_next(buf);
-                if (asked < total) request_next(buf + 1 == NBUF ? 0 : buf + 1);
+                ring.fill(buf, NBUF - 1);
                 __builtin_amdgcn_s_waitcnt(vm_wait(0));
                 __syncthreads();
             }
@@ -536,17 +503,17 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a)
 template <int D, bool F16>
 hipError_t launch(const CrossArgs& a, hipStream_t stream)
 {
-    const unsigned grid = cross_grid((long long)a.slots * a.parts, a.K, a.turn), threads = 64 * RowStage<D>::WAVES, few_threads = 64 * FewStage<D>::WAVES;
+    const unsigned grid = cross_grid((long long)a.slots * a.parts, a.K, a.turn), few_threads = 64 * FewStage<D>::WAVES;
     const bool split = a.parts > 1;
     if (a.few) {
         if (split) k_cross_few<D, F16, true><<<grid, few_threads, 0, stream>>>(a);
         else k_cross_few<D, F16, false><<<grid, few_threads, 0, stream>>>(a);
     } else if (split) {
-        if (a.lse) k_cross<D, F16, true, true><<<grid, threads, 0, stream>>>(a);
-        else k_cross<D, F16, true, false><<<grid, threads, 0, stream>>>(a);
+        if (a.lse) k_cross<D, F16, true, true><<<grid, 256, 0, stream>>>(a);
+        else k_cross<D, F16, true, false><<<grid, 256, 0, stream>>>(a);
     } else {
-        if (a.lse) k_cross<D, F16, false, true><<<grid, threads, 0, stream>>>(a);
-        else k_cross<D, F16, false, false><<<grid, threads, 0, stream>>>(a);
+        if (a.lse) k_cross<D, F16, false, true><<<grid, 256, 0, stream>>>(a);
+        else k_cross<D, F16, false, false><<<grid, 256, 0, stream>>>(a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !split) return e;
@@ -570,7 +537,7 @@ CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_
     CrossPlan p = {};
     const long long rows = n_q * group;               // of one key/value head
     p.few = max_q * group <= 32 && !backward;
-    const int block_shift = p.few ? 5 : head_dim == 128 ? 8 : 7;   // one wave's tile, or that of eight or four waves
+    const int block_shift = p.few ? 5 : 7;            // the tile of one wave, or of four
     // fewer than two workgroups per compute unit: parts of 256 keys at least, until there are about three
     long long work = (rows + (1ll << block_shift) - 1) >> block_shift;
     if (work < segments) work = segments;

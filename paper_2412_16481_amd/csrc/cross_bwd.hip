@@ -15,6 +15,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "cross_common.h"
 
 namespace f3d {
@@ -48,12 +50,12 @@ __device__ __forceinline__ void store_row(float* part, uint16_t* to, const f32x1
 // Runs of row blocks, stages and their hand-over as in the forward kernel. Per tile of 32 keys a wave has 2 KS MFMAs for the scores and dP
 // (of the NEXT tile, issued between the exponentials of the current one; -D is the accumulator dP starts from) and 2 MT for dQ.
 template <int D, bool SPLIT>
-__global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross_bwd_dq(CrossBwdArgs b)
+__global__ __launch_bounds__(256, 2) void k_cross_bwd_dq(CrossBwdArgs b)
 {
     using T = Tile<D>;
     using S = RowStage<D>;
-    constexpr int KS = T::KS, MT = T::MT, LPW = S::LPW, NBUF = S::NBUF, NW = S::WAVES;
-    constexpr int BM = 32 * NW;
+    constexpr int KS = T::KS, MT = T::MT, NBUF = S::NBUF;
+    constexpr int BM = 128;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::TOTAL];
     const CrossArgs& a = b.f;
     const uint32_t sK = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
@@ -76,43 +78,15 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross_bwd_dq(Cro
     const int nkeys = first_row >= live ? 0 : SPLIT ? min(max(kv.len - key0, 0), a.chunk) : kv.len;
 
     const uint32_t row_bytes = (uint32_t)a.K * T::ROWB;
-    const uint64_t first = (uint64_t)(kv.from + key0) * row_bytes + (uint64_t)kh * T::ROWB;
-    int srow[LPW];
-    uint32_t scol[LPW];
-#pragma unroll
-    for (int i = 0; i < LPW; ++i) {
-        const int p = (wave * LPW + i) * 64 + lane;
-        srow[i] = p / T::NC;
-        scol[i] = ((p % T::NC) ^ T::swizzle(srow[i])) << 4;
-    }
-    const int nst = (nkeys + S::ROWS - 1) / S::ROWS;
-    const bool stays = nst <= NBUF;
-    const int total = stays ? nst : nst * blocks;
-    int asked = 0, ask_st = 0;
-    auto request_next = [&](int buf) __attribute__((always_inline)) {
-        const uint32_t to = buf * S::BYTES;
-#pragma unroll
-        for (int i = 0; i < LPW; ++i) {
-            const int key = min(ask_st * S::ROWS + srow[i], nkeys - 1);
-            const uint64_t at = first + (uint64_t)(uint32_t)key * row_bytes + scol[i];
-            lds_dma16(reinterpret_cast<const char*>(a.k) + at, sK + to + (wave * LPW + i) * 1024);
-            lds_dma16(reinterpret_cast<const char*>(a.v) + at, sK + KV + to + (wave * LPW + i) * 1024);
-        }
-        ++asked;
-        ask_st = ask_st + 1 == nst ? 0 : ask_st + 1;
-    };
-    if (total > 0) request_next(0);
-    if (total > 1) request_next(1);
-#pragma unroll
-    for (int i = 2; i < NBUF; ++i)
-        if (stays && total > i) request_next(i);
+    KeyRing<D> ring;
+    ring.start(a.k, a.v, (uint64_t)(kv.from + key0) * row_bytes + (uint64_t)kh * T::ROWB, row_bytes, nkeys, blocks, sK, wave);
 
     uint32_t off[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) off[ks] = sK + T::row_piece(lane, ks);
     const uint32_t toff = sK + T::transposed(lane);
     const float mul = a.s_mul;
-    if (total > 0) {
+    if (nkeys > 0) {
         __builtin_amdgcn_s_waitcnt(vm_wait(0));
         __syncthreads();
     }
@@ -171,7 +145,7 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross_bwd_dq(Cro
     };
 
     f32x16 sa, sb, da, db;
-    int buf = 0;
+    int buf = 0, read = 0;                            // read: stages over all row blocks
     // A block's rows are asked for a block ahead, where the registers allow it
     constexpr bool AHEAD = D <= 64;
     U4 nq[KS], ng[KS], no[KS];
@@ -217,8 +191,8 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross_bwd_dq(Cro
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16{0};
         }
-        if (stays) buf = 0;
-        if (nst > 0 && busy) {
+        if (ring.stays) buf = 0;
+        if (nkeys > 0 && busy) {
             sa = f32x16{0};
             da = minus_d;
 #pragma unroll
@@ -230,23 +204,25 @@ __global__ __launch_bounds__(64 * RowStage<D>::WAVES, 2) void k_cross_bwd_dq(Cro
                 da = mfma(vf, gf[ks], da);
             }
         }
-        for (int st = 0; st < nst; ++st) {
+        auto stage = [&](int st, auto first_tile) __attribute__((always_inline)) {
             const int bufn = buf + 1 == NBUF ? 0 : buf + 1;
             const uint32_t at0 = buf * S::BYTES, an0 = bufn * S::BYTES;
 #pragma unroll
             for (int t4 = 0; t4 < S::TILES; ++t4) {
-                if (t4 + 1 == S::TILES && !stays) {   // the hand-over of the forward kernel
-                    __builtin_amdgcn_s_waitcnt(vm_wait(0));
-                    __syncthreads();
-                    if (asked < total) request_next(bufn + 1 == NBUF ? 0 : bufn + 1);
-                }
+                if (t4 + 1 == S::TILES && !ring.stays) ring.hand_over(buf, ++read);
                 const int kbase = st * S::ROWS + t4 * 32;
                 if (!busy || kbase >= nkeys) continue;
                 const uint32_t at = at0 + t4 * T::BYTES, an = t4 + 1 < S::TILES ? at + T::BYTES : an0;
-                if ((t4 & 1) == 0) unit(sa, da, at, kbase, sb, db, an);
+                if (((t4 + decltype(first_tile)::value) & 1) == 0) unit(sa, da, at, kbase, sb, db, an);
                 else unit(sb, db, at, kbase, sa, da, an);
             }
             buf = bufn;
+        };
+        for (int st = 0; st < ring.nst; st += S::LOOP) {
+            stage(st, std::integral_constant<int, 0>{});
+            if (S::LOOP == 1) continue;
+            if (st + 1 >= ring.nst) break;
+            stage(st + 1, std::integral_constant<int, 1>{});
         }
         if (row >= rows) continue;
         const int i = divide(row, a.G, a.by_g), g = row - i * a.G;
@@ -726,9 +702,8 @@ hipError_t launch(const CrossBwdArgs& b, hipStream_t stream)
     }
     if (a.n_q > 0) {
         const unsigned grid = cross_grid((long long)a.slots * a.parts, a.K, a.turn);
-        constexpr int THREADS = 64 * RowStage<D>::WAVES;
-        if (a.parts > 1) k_cross_bwd_dq<D, true><<<grid, THREADS, 0, stream>>>(b);
-        else k_cross_bwd_dq<D, false><<<grid, THREADS, 0, stream>>>(b);
+        if (a.parts > 1) k_cross_bwd_dq<D, true><<<grid, 256, 0, stream>>>(b);
+        else k_cross_bwd_dq<D, false><<<grid, 256, 0, stream>>>(b);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (a.parts > 1) {

@@ -144,20 +144,89 @@ __device__ __forceinline__ void zero_rows(uint16_t* x, int n, int from, int to, 
         reinterpret_cast<uint4*>(x)[i < head ? i : tail + (i - head)] = make_uint4(0, 0, 0, 0);
 }
 
-// Keys and values in LDS for the kernels whose waves own query rows: stages of ROWS keys, NBUF of them resident.
+constexpr int vm_wait(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }   // s_waitcnt operand: the memory counter alone
+
+// Keys and values in LDS for the kernels whose waves own query rows: stages of ROWS keys, NBUF of them resident. At 128 channels a stage
+// is one tile, so that two workgroups fit on a compute unit; loops go over two of them then (LOOP: stages, together an even number of tiles).
 template <int D>
 struct RowStage {
     using T = Tile<D>;
-    static constexpr int WAVES = D == 128 ? 8 : 4;    // 128: three stages leave room for one workgroup on a compute unit
-    static constexpr int ROWS = D == 16 ? 128 : 64;
+    static constexpr int ROWS = D == 16 ? 128 : D == 128 ? 32 : 64;
     static constexpr int TILES = ROWS / 32;
+    static constexpr int LOOP = TILES == 1 ? 2 : 1;
     static constexpr int BYTES = ROWS * T::ROWB;      // of K, and of V
-    static constexpr int NBUF = D == 32 ? 4 : 3;
-    static constexpr int LPW = ROWS * T::NC / (64 * WAVES);
+    static constexpr int NBUF = D == 32 || D == 128 ? 4 : 3;
+    static constexpr int LPW = ROWS * T::NC / 256;    // loads per lane, stage and tensor
     static constexpr int TOTAL = NBUF * 2 * BYTES;
 };
 
-constexpr int vm_wait(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }   // s_waitcnt operand: the memory counter alone
+// The keys of a workgroup of four waves on their way through LDS: K of buffer b at b BYTES from `lds` on, V NBUF BYTES further on. Where
+// they fit they are staged once and stay; else stage after stage, over and over for the row blocks of a run, each NBUF - 1 stages
+// before it is read.
+template <int D>
+struct KeyRing {
+    using T = Tile<D>;
+    using S = RowStage<D>;
+    const char* k;
+    const char* v;
+    uint32_t lds, row_bytes;
+    int nkeys, nst, total, asked, next, wave;         // total, asked: stages over all row blocks; next: the keys of the one to ask for
+    bool stays;
+    int srow[S::LPW];
+    uint32_t scol[S::LPW];
+
+    __device__ __forceinline__ void start(const uint16_t* keys, const uint16_t* values, uint64_t first, uint32_t pitch, int n, int blocks, uint32_t at, int w)
+    {
+        k = reinterpret_cast<const char*>(keys) + first;
+        v = reinterpret_cast<const char*>(values) + first;
+        lds = at;
+        row_bytes = pitch;
+        nkeys = n;
+        wave = w;
+        nst = (n + S::ROWS - 1) / S::ROWS;
+        stays = nst <= S::NBUF;
+        total = stays ? nst : nst * blocks;
+        asked = next = 0;
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < S::LPW; ++i) {
+            const int p = (wave * S::LPW + i) * 64 + lane;
+            srow[i] = p / T::NC;
+            scol[i] = ((p % T::NC) ^ T::swizzle(srow[i])) << 4;
+        }
+        fill(0, stays ? S::NBUF : S::NBUF - 1);
+    }
+    __device__ __forceinline__ void request(int buf)
+    {
+#pragma unroll
+        for (int i = 0; i < S::LPW; ++i) {
+            const int key = min(next * S::ROWS + srow[i], nkeys - 1);   // past the end: the last key again
+            const uint64_t at = (uint64_t)(uint32_t)key * row_bytes + scol[i];
+            const uint32_t to = lds + buf * S::BYTES + (wave * S::LPW + i) * 1024;
+            lds_dma16(k + at, to);
+            lds_dma16(v + at, to + S::NBUF * S::BYTES);
+        }
+        ++asked;
+        next = next + 1 == nst ? 0 : next + 1;
+    }
+    // the next `n` stages, as far as there are any, to the buffers from `buf` on
+    __device__ __forceinline__ void fill(int buf, int n)
+    {
+        for (int i = 0; i < n && asked < total; ++i) {
+            request(buf);
+            buf = buf + 1 == S::NBUF ? 0 : buf + 1;
+        }
+    }
+    // In the last tile of the stage in buffer `buf`, `read` stages before it: the next one is handed over to the readers, and the buffer
+    // of the one before this is asked for again. Whoever arrives has its own loads of the next stage and has read the one before this.
+    __device__ __forceinline__ void hand_over(int buf, int read)
+    {
+        if (S::NBUF > 3 && asked - read > 1) __builtin_amdgcn_s_waitcnt(vm_wait((S::NBUF - 3) * 2 * S::LPW));   // but the stages behind it
+        else __builtin_amdgcn_s_waitcnt(vm_wait(0));
+        __syncthreads();
+        if (asked < total) request(buf == 0 ? S::NBUF - 1 : buf - 1);
+    }
+};
 
 }  // namespace
 
