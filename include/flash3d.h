@@ -371,8 +371,8 @@ int f3d_layer_norm(const void *x, const int32_t *row_in, const float *gamma, con
  *     dx[r] = rstd[p] * (g - mean(g) - xh * mean(g * xh)) + residual[r],   dgamma = sum_p dy[p] * xh,   dbeta = sum_p dy[p]
  *   dy          `dtype` [n, channels], row p as in y;  x, row_in, gamma, n, channels, dtype  as in the forward call
  *   mean, rstd  binary32 [n], the forward call's
- *   row_in      NULL or a permutation of the rows of x: dx is stored where x was read. Of a row that is named twice one of the two
- *               results is kept, a row that is not named keeps what dx held
+ *   row_in      NULL or [n] int32, every row named once at most: dx is stored where x was read. A row that is not named keeps what
+ *               dx held
  *   residual    NULL or `dtype` [n, channels], indexed by the DESTINATION row: the gradient that reaches x past the norm
  *   dx   (out)  `dtype` [n, channels]; may be residual, and dy or x where row_in is NULL
  *   dgamma, dbeta (out)  binary32 [channels], either may be NULL; zeros for n = 0
@@ -396,7 +396,7 @@ int f3d_layer_norm_bwd(const void *dy, const void *x, const int32_t *row_in, con
  *   norm (out)  binary32 [1]
  *   workspace   >= f3d_clip_grads_workspace_bytes(n_tensors), 256-byte aligned. The host arrays may go when the call returns
  * Squares and sums are held in binary64 and added in a fixed order: no finite gradient overflows, the same call gives the same bits.
- * A norm that is infinite scales by 0 and one that is NaN by NaN.
+ * A norm that is infinite scales by 0 and one that is NaN by NaN, but with max_norm infinite nothing is scaled.
  */
 #define F3D_CLIP_MAX_TENSORS 65536
 int f3d_clip_grads_workspace_bytes(int32_t n_tensors, size_t *out_bytes);

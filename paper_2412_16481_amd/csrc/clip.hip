@@ -188,7 +188,8 @@ __global__ __launch_bounds__(CTH) void k_clip_scale(const ClipTensor* table, int
     const double norm = sqrt(block_sum(s, box));
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     double ratio = (double)max_norm / (norm + 1e-6);
-    if (ratio > 1.0) ratio = 1.0;                     // a norm that is no number stays one in every gradient
+    // a norm that is no number stays one in every gradient; no norm is longer than an infinite largest one
+    if (ratio > 1.0 || isinf(max_norm)) ratio = 1.0;
     Factor c = {(float)ratio, 1.0f};
     if (ratio < 0x1p-120) c = {(float)(ratio * 0x1p64), 0x1p-64f};
     for (int k = blockIdx.x; k < chunks; k += gridDim.x) {

@@ -324,6 +324,18 @@ def test_clip_grads_infinities_and_nan():
         assert bool((rest == 0).all()) if others == 0.0 else bool(rest.isnan().all())
 
 
+def test_clip_grads_with_an_infinite_largest_norm_scales_nothing():
+    for bad in (math.inf, math.nan):
+        grads = [torch.ones(100, device=DEV), torch.ones(70000, dtype=torch.bfloat16, device=DEV)]
+        grads[0][3] = bad
+        outs = [torch.zeros_like(g) for g in grads]
+        for to in (None, outs):
+            norm = float(f3d.clip_grads(grads, math.inf, outs=to))
+            assert norm == math.inf if bad == math.inf else math.isnan(norm)
+        for got in (grads, outs):
+            assert got[0].isfinite().sum() == 99 and bool((got[1] == 1).all())
+
+
 def test_clip_grads_outputs_may_be_some_of_the_gradients():
     _, grads = clip_case([100, 5000, 33], ("f32", "bf16"))
     want, outs = check_clip(grads, 0.2, False)
