@@ -288,8 +288,8 @@ int f3d_bucket_swin_attn_bwd(const void *q, const void *k, const void *v, const 
  * Inconsistent offsets or lengths give unspecified results but no access out of bounds. out overlaps no input.
  * Arithmetic: 16-bit operands, fp32 accumulation and softmax, the sum of the exponentials taken in fp32, the probabilities rounded to 16
  * bits before the product with v; one rounding of the result. Inputs must be finite, and so must the products q k^T and their scaled
- * values in binary32. The same call gives the same bits; how the keys are split follows from n_q, n_segments,
- * max_q, max_kv, heads, kv_heads and head_dim.
+ * values in binary32; values of v above 2^80 in magnitude may overflow, those below 2^-80 may count as zeros. The same call gives the
+ * same bits; how the keys are split follows from n_q, n_segments, max_q, max_kv, heads, kv_heads and head_dim.
  */
 int f3d_cross_attn_workspace_bytes(int64_t n_q, int64_t n_kv, int32_t n_segments, int64_t max_q, int64_t max_kv, int32_t heads,
                                    int32_t kv_heads, int32_t head_dim, size_t *out_bytes);
@@ -309,7 +309,7 @@ int f3d_cross_attn_f16(const void *q, const void *k, const void *v, const int32_
  * Backward of f3d_cross_attn:
  *     P = exp(S - lse),  dP = dout v^T,  D = rowsum(dout o out),  dS = P o (dP - D),
  *     dq = scale dS k,   dk = scale sum over the heads that share it of dS^T q,   dv = the same sum of P^T dout
- *   q .. softmax_scale   as in the forward call;  out, dout  bf16 [n_q, heads*head_dim];  lse  the forward call's
+ *   q .. softmax_scale   as in the forward call, a scale below 2^-100 is refused;  out, dout  bf16 [n_q, heads*head_dim];  lse  the forward call's
  *   dq (out)  bf16 [n_q, heads*head_dim];  dk, dv (out)  bf16 [n_kv, kv_heads*head_dim]. Rows behind a segment's length get zeros, and
  *             so do rows of no segment and everything of a segment without queries or without keys. The gradients overlap no input and
  *             not each other

@@ -184,7 +184,7 @@ __global__ __launch_bounds__(256, 2) void k_cross_bwd_dq(CrossBwdArgs b)
             }
             dot += __shfl_xor(dot, 32, 64);
             if (takes && part == 0 && hf == 0) b.dsum[place] = dot;
-            nl = takes && nkeys > 0 ? -LOG2E * nlse : -1e30f;   // rows that take no part: probabilities exactly zero
+            nl = takes && nkeys > 0 ? -LOG2E * nlse : -INFINITY;   // rows that take no part: probabilities exactly zero
             if (AHEAD && blk + 1 < blocks) fetch_row(blk + 1);
 #pragma unroll
             for (int r2 = 0; r2 < 16; ++r2) minus_d[r2] = -dot;
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(256, 2) void k_cross_bwd_dq(CrossBwdArgs b)
 // The query rows stream through LDS in stages of KStage::ROWS, three of them resident. Per tile of 32 rows a wave has 4 KS MFMAs for the
 // scores and dP (of the NEXT tile: they are issued between the exponentials of the current one) and 4 MT for the two gradients. The
 // starting accumulators of a tile are read from LDS: -lse (in the score's units) and -D of its rows, so neither costs a
-// subtraction, and rows past the end have -1e30 there: their probabilities are exactly zero.
+// subtraction, and rows past the end have -infinity there: their probabilities are exactly zero.
 template <int D>
 struct KStage {
     using T = Tile<D>;
@@ -248,7 +248,7 @@ struct KStage {
 };
 
 template <int D, bool SPLIT>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossBwdArgs b)
+__global__ __launch_bounds__(256, 2) void k_cross_bwd_dkdv(CrossBwdArgs b)
 {
     using T = Tile<D>;
     using S = KStage<D>;
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void k_cross_bwd_dkdv(CrossB
             const int q = divide(rc, a.G, a.by_g), g = rc - q * a.G;
             const size_t at = (size_t)(qs.from + q) * a.H + kh * a.G + g;
             const float l = a.lse[at], d = b.dsum[at];
-            nl = r < nrows ? l * lmul : -1e30f;
+            nl = r < nrows ? l * lmul : -INFINITY;
             nd = -d;
         }
 #pragma unroll
@@ -505,7 +505,7 @@ __global__ __launch_bounds__(512, 2) void k_cross_bwd_dkdv_wide(CrossBwdArgs b)
             const int q = divide(rc, a.G, a.by_g), g = rc - q * a.G;
             const size_t at = (size_t)(qs.from + q) * a.H + kh * a.G + g;
             const float l = a.lse[at], d = b.dsum[at];
-            nl = r < nrows ? l * lmul : -1e30f;
+            nl = r < nrows ? l * lmul : -INFINITY;
             nd = -d;
         }
 #pragma unroll

@@ -186,7 +186,7 @@ __global__ __launch_bounds__(256, 2) void k_cross_bwd_short(CrossBwdArgs b)
         int nk = nkeys;
         asm volatile("" : "+s"(keys), "+s"(nk));
         const float lse = *(const __attribute__((address_space(3))) float*)(uintptr_t)(own + LSE + buf * 128 + l32 * 4);
-        const float nl = row < live ? -LOG2E * lse : -1e30f;   // rows that take no part: probabilities exactly zero
+        const float nl = row < live ? -LOG2E * lse : -INFINITY;   // rows that take no part: probabilities exactly zero
         f32x16 minus_d, dq = f32x16{0}, s, dp;
 #pragma unroll
         for (int r = 0; r < 16; ++r) minus_d[r] = -dot;

@@ -10,10 +10,10 @@ namespace {
 
 template <bool F16>
 struct Half {
-    // Bounds of a sum of exponentials taken against the reference 0. bfloat16: none overflowed, and the largest is far above the
-    // flush-to-zero range. binary16: a probability above 65504 rounds to infinity, and what is lost of those below 2^-14 stays below
-    // 2^-25 a key of the sum.
-    static constexpr float SUM_LO = F16 ? 1.0f : 0x1p-40f, SUM_HI = F16 ? 65504.f : 0x1p80f;
+    // Bounds of a sum of exponentials taken against the reference 0. bfloat16: binary32 has room for the products with values of 2^80 on
+    // either side. binary16: a probability above 65504 rounds to infinity, and what is lost of those below 2^-14 stays below 2^-25 a
+    // key of the sum.
+    static constexpr float SUM_LO = F16 ? 1.0f : 0x1p-40f, SUM_HI = F16 ? 65504.f : 0x1p40f;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi)
     {
         if constexpr (F16) {

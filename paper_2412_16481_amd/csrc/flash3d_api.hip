@@ -796,6 +796,7 @@ int f3d_cross_attn_bwd(const void* q, const void* k, const void* v, const void* 
     memset(&b, 0, sizeof(b));
     rc = fill_cross_args(b.f, s, p, q, k, v, q_offsets, kv_offsets, q_lens, kv_lens, softmax_scale, 0, &b.scale);
     if (rc != F3D_OK) return rc;
+    if (b.scale < 0x1p-100f) return F3D_ERR_UNSUPPORTED;   // lse / scale has to be finite
     if (n_q == 0 && n_kv == 0) return F3D_OK;
     if ((n_q > 0 && (!out || !dout || !lse || !dq)) || (n_kv > 0 && (!dk || !dv))) return F3D_ERR_INVALID_ARG;
     if (((uintptr_t)out | (uintptr_t)dout | (uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv) & 15 || (uintptr_t)lse & 3) return F3D_ERR_BAD_ALIGNMENT;

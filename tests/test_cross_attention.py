@@ -269,6 +269,75 @@ def test_cross_attention_scales_and_sharp_scores(D, t):
             check_forward(d, out, lse, scale)
 
 
+@pytest.mark.parametrize("D", [16, 32, 64, 128])
+def test_cross_attention_gradients_at_the_smallest_scale(D):
+    # every probability is 1 / n; rows that only fill a tile up must not count, however small their scaled scores are
+    check_backward(make([70, 3], [200, 33], 4, 2, D, "bf16"), scale=2.0 ** -100)
+    check_backward(make([70, 3], [90, 33], 4, 2, D, "bf16"), scale=2.0 ** -100)
+
+
+@pytest.mark.parametrize("D", [16, 64, 128])
+@pytest.mark.parametrize("kv", [100, 700])
+def test_cross_attention_values_as_large_as_they_may_be(D, kv):
+    # scores about 45 above the others: exponentials of 2^65, times values of 2^79
+    d = make([200], [kv], 2, 1, D, "bf16", q_scale=0.05)
+    d["q"] += 4.0
+    d["k"] *= 0.05
+    d["k"][kv // 2] = 45.0 / math.sqrt(D) / 4
+    for power in (79, -70):
+        e = {**d, "v": (d["v"].float() * 2.0 ** power).to(torch.bfloat16)}
+        out, lse = forward(e)
+        check_forward(e, out, lse)
+
+
+# a workgroup takes a run of two to eight row blocks here; keys that stay in LDS and keys that stream
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("kv", [90, 700])
+@pytest.mark.parametrize("D,H,n", [(16, 16, 200000), (32, 8, 200003), (128, 2, 400000)])
+def test_cross_attention_runs_of_blocks_some_of_which_are_sharp(D, H, n, kv, t):
+    g = torch.Generator(device=DEV).manual_seed(n + D + kv)
+    r = lambda rows: torch.randn(rows, H * D, generator=g, device=DEV)   # noqa: E731
+    q, k, v = r(n), r(kv).to(TYPES[t]), r(kv).to(TYPES[t])
+    sharp = [0, 130, 511, 1023, 1024, 128 * 31 + 5, n // 2, n - 300, n - 1]
+    q[sharp] *= 60
+    rows = sorted(set(sharp + [x + i for x in sharp for i in (-128, -1, 1, 64, 128) if 0 <= x + i < n] + list(range(7, n, n // 200))))
+    q = q.to(TYPES[t])
+    lse = torch.empty(n, H, device=DEV)
+    out = f3d.cross_attn(q, k, v, None, None, H, D, lse=lse)
+    part = {"q": q[rows].contiguous(), "k": k, "v": v, "q_off": ends([len(rows)]), "kv_off": ends([kv]), "q_len": [len(rows)], "kv_len": [kv], "H": H, "K": H,
+            "D": D, "t": TYPES[t]}
+    check_forward(part, out[rows], lse[rows])
+    plain = f3d.cross_attn(q, k, v, None, None, H, D)                   # without lse: another form of the kernel
+    assert torch.equal(plain, out)
+    if t == "f16":
+        return
+    dout = (0.1 * r(n)).to(TYPES[t])
+    dq, _, _ = f3d.cross_attn_bwd(q, k, v, out, dout, lse, None, None, H, D)
+    for h in range(H):
+        col = slice(h * D, (h + 1) * D)
+        _, kk, s, e = scores(part, slice(0, len(rows)), slice(0, kv), h, h, 1 / math.sqrt(D))
+        vv, do, o = v[:, col].double(), dout[rows, col].double(), out[rows, col].double()
+        p = torch.exp(s - lse[rows, h].double()[:, None])
+        ds = p * (do @ vv.T - (do * o).sum(1, keepdim=True))
+        off = (D + 8) * U * (do.abs() @ vv.abs().T + (do * o).abs().sum(1, keepdim=True))
+        e2 = 2 * e + 4 * U * (1 + lse[rows, h].double().abs()[:, None])
+        b = half(TYPES[t])
+        room = (ds.abs() * (b + e2) * (1 + b) + p * off + (kv + 8) * U * ds.abs()) @ kk.abs() / math.sqrt(D)
+        want = ds @ kk / math.sqrt(D)
+        close(dq[rows, col], want, room * (1 + b) + (b + U) * want.abs() + least(TYPES[t]), f"dq, head {h}")
+
+
+@pytest.mark.parametrize("D,kv", [(16, n) for n in (1, 31, 32, 33, 64, 65, 95, 96, 97, 128, 129)] + [(32, n) for n in (1, 31, 32, 33, 64, 65, 95, 96, 97)])
+def test_cross_attention_gradients_of_few_keys(D, kv):
+    # segments of many rows, whose sums are split, beside short ones, and a padded batch in which rows and keys are missing
+    d = make([1500, 1, 0, 129], [kv, max(kv - 1, 0), 1, kv], 4, 2, D, "bf16")
+    check_backward(d)
+    for name, rows in (("q", slice(400, 1500)), ("k", slice(kv // 2, kv))):
+        d[name][rows] = math.nan                                        # behind the lengths
+    d["v"][kv // 2:kv] = math.nan
+    check_backward(d, q_lens=[400, 1, 0, 100], kv_lens=[kv // 2, max(kv - 1, 0), 0, kv])
+
+
 def test_cross_attention_one_key_returns_its_value():
     # the probability is exactly one
     d = make([10, 200, 1], [1, 1, 1], 4, 2, 64, "bf16", q_scale=3.0)

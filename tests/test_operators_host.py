@@ -119,6 +119,7 @@ def test_cross_attn_refuses(kw, code):
 @pytest.mark.parametrize("kw,code", SHARED + [
     (dict(workspace=None), INVALID), (dict(workspace=AT + 128), ALIGN), (dict(workspace_bytes=100 * 8 * 4 - 1), SMALL), (dict(dout=None), INVALID),
     (dict(lse=None), INVALID), (dict(dq=None), INVALID), (dict(dk=None), INVALID), (dict(dv=None), INVALID), (dict(dk=AT + 4), ALIGN),
+    (dict(scale=2.0 ** -101), UNSUPPORTED),
     (dict(n_q=0, n_kv=0, q=None, k=None, v=None, out=None, workspace=None), OK)])
 def test_cross_attn_bwd_refuses(kw, code):
     assert cross_bwd(**kw) == code
