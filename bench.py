@@ -139,9 +139,12 @@ def main() -> int:
                     help="also time f3d_inbucket_pool (mean, tiles of 1024 rows, this reduction factor) on the attention output")
     ap.add_argument("--backward", action="store_true",
                     help="also time f3d_bucket_swin_attn_bwd (after a forward that stores the log-sum-exp) for every pass")
+    ap.add_argument("--train", type=int, default=0, metavar="RHO",
+                    help="also time a training step of a block whose points attend to the pooled points of their scan (tiles of 1024 rows, "
+                         "this reduction factor): layer norm, f3d_cross_attn, both backward passes, the clipping of all gradients")
     ap.add_argument("--dtype", default="bf16", choices=["bf16", "f16"],
                     help="element type of q, k, v and the output: bf16 (the benchmark configurations) or f16 (the "
-                         "Appendix's FP16 features; forward path only, not with --pool/--backward/--glue)")
+                         "Appendix's FP16 features; forward path only, not with --pool/--backward/--train/--glue)")
     ap.add_argument("--bucketize-scale", type=int, default=0, metavar="SCANS",
                     help="also time f3d_psh_bucketize alone on SCANS uniform-cube scans of 131072 points each (its "
                          "bandwidth regime: the five configurations are too small to load the memory system)")
@@ -176,7 +179,7 @@ def main() -> int:
     coords = torch.from_numpy(w.coords).to(dev)
     bo = torch.from_numpy(w.batch_offsets).to(dev)
     gen = torch.Generator(device=dev).manual_seed(w.seed)
-    if args.dtype == "f16" and (args.pool or args.backward or args.glue):
+    if args.dtype == "f16" and (args.pool or args.backward or args.train or args.glue):
         sys.exit("bench.py: --dtype f16 covers the forward path only")
     # the seeded N(0,1) features of the workload, the same arrays the parity tests feed to both sides (bf16 bit
     # patterns; for --dtype f16 the same values rounded to binary16)
@@ -415,6 +418,48 @@ def main() -> int:
                            "roofline": {"bound": "mfma", "achieved": mean_tf, "peak": PEAK_BF16_TFLOPS, "unit": "TFLOP/s",
                                         "frac": mean_tf / PEAK_BF16_TFLOPS},
                            "note": "algorithmic FLOP = 2.5 x forward; where two kernels run, both compute S and dP, which counts once"}
+    if args.train > 0:   # layer norm, attention to the pooled points and the gradients of both, outside the headline step
+        pooled = f3d.inbucket_pool(coords, bk.perm, out, bo, 1024, args.train, 0.1, args.hash, "mean")
+        kv_off = pooled.pooled_offsets
+        kv_rows = np.diff(kv_off.cpu().numpy())
+        n_kv, max_kv = int(kv_rows.sum()), int(kv_rows.max())
+        keys = pooled.feat[:n_kv].contiguous()
+        feat = torch.randn(n, C, device=dev, generator=gen, dtype=torch.float32).to(torch.bfloat16)
+        dres = torch.randn(n, C, device=dev, generator=gen, dtype=torch.float32).to(torch.bfloat16)
+        gamma, beta = torch.ones(C, device=dev), torch.zeros(C, device=dev)
+        mean, rstd, lse = torch.empty(n, device=dev), torch.empty(n, device=dev), torch.empty(n, H, device=dev)
+        y, att = torch.empty_like(feat), torch.empty_like(feat)
+
+        def train_step(mark):
+            mark()
+            f3d.layer_norm(feat, gamma, beta, 1e-5, bk.perm, out=y, mean=mean, rstd=rstd)
+            mark()
+            f3d.cross_attn(y, keys, keys, bo, kv_off, H, d, H, max_scan, max_kv, out=att, lse=lse)
+            mark()
+            dq, dk, dv = f3d.cross_attn_bwd(y, keys, keys, att, dres, lse, bo, kv_off, H, d, H, max_scan, max_kv)
+            mark()
+            dx, dgamma, dbeta = f3d.layer_norm_bwd(dq, feat, mean, rstd, gamma, bk.perm, dres)
+            mark()
+            f3d.clip_grads([dx, dk, dv, dgamma, dbeta], 1.0)
+            mark()
+
+        train_step(lambda: None)
+        torch.cuda.synchronize()
+        marks = []
+
+        def mark():
+            marks.append(torch.cuda.Event(enable_timing=True))
+            marks[-1].record()
+        for _ in range(args.steps):
+            train_step(mark)
+        torch.cuda.synchronize()
+        names = ("layer_norm", "cross_attn", "cross_attn_bwd", "layer_norm_bwd", "clip_grads")
+        ms = {name: float(np.mean([marks[6 * i + j].elapsed_time(marks[6 * i + j + 1]) for i in range(args.steps)])) for j, name in enumerate(names)}
+        pairs = float((np.diff(w.batch_offsets).astype(np.float64) * kv_rows).sum())   # of a query row and a key
+        fwd, by_norm, by_bwd = 4.0 * pairs * C, n * (4 * C + 12), n * (8 * C + 12)     # rows and statistics; the residual's gradient too
+        res["train"] = {"rho": args.train, "pooled_rows": n_kv, "ms": sum(ms.values()), "points_per_s": n / (sum(ms.values()) * 1e-3), "parts_ms": ms,
+                        "cross_attn_tflops": fwd / ms["cross_attn"] / 1e9, "cross_attn_bwd_tflops": 2.5 * fwd / ms["cross_attn_bwd"] / 1e9,
+                        "layer_norm_gbps": by_norm / ms["layer_norm"] / 1e6, "layer_norm_bwd_gbps": by_bwd / ms["layer_norm_bwd"] / 1e6}
     if args.glue:
         feat = torch.randn(n, C, device=dev, generator=gen, dtype=torch.float32).to(torch.bfloat16)
         wqkv = (torch.randn(3 * C, C, device=dev, generator=gen, dtype=torch.float32) / C ** 0.5).to(torch.bfloat16)
