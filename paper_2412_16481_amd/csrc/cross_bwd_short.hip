@@ -9,7 +9,8 @@
 //   dV^T += dO^T P, dK^T += Q^T dS   P and dS go through LDS (32 x 32 each) and come back transposed: a lane then owns one KEY, and the rows
 //                                    are in the order in which the transposing read delivers Q^T and dO^T.
 // The waves of a workgroup add up their sums at the end, in order; a segment's rows are split over workgroups whose sums the join of
-// cross_bwd.hip adds up.
+// cross_bwd.hip adds up. Bound: the vector ALU's issue port (exponentials, packing) and LDS. 200000 rows, 77 keys, 4 x 16 channels: 44 us
+// with the join, where the two kernels of cross_bwd.hip take 93. 128 keys of 32 channels would need more registers and LDS than two workgroups have.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -81,7 +81,8 @@ __device__ __forceinline__ int segment_of(const int32_t* offsets, int n, int seg
 
 // Which piece of work is this workgroup's. Workgroups go to the eight XCDs in turn; each XCD takes `turn` consecutive pieces, then the
 // next eight turns follow: neighbours, which read the same keys (or rows), share an L2, and segments of different lengths are still
-// spread over all of them. (One eighth of all pieces to each XCD: 16 ragged segments, 64 channels, TAG_US.)
+// spread over all of them. (16 ragged segments of up to 2047 rows and 1500 keys, 12 heads of 64 channels: 120 us, and 149 with one eighth
+// of all pieces to each XCD, which leaves the XCDs of the short segments idle.)
 __device__ __forceinline__ uint32_t piece_of(uint32_t turn)
 {
     const uint32_t i = blockIdx.x >> 3, round = i / turn;

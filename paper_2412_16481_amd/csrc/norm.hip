@@ -11,6 +11,9 @@
 // The backward's teams keep their columns from row to row, so the sums of the weights' gradients stay in registers
 // too; a workgroup adds up its teams at its end and leaves 2 c sums in the workspace, which a second launch adds up in a fixed
 // order: the same call gives the same bits.
+//
+// Bound: HBM. Measured: 914601 rows of 256 bfloat16 channels forward 176 us = 5.3 TB/s, backward with a residual and the weights' gradients
+// 381 us = 4.9 TB/s; 9001 rows of 1537 binary32 channels, which no 16-byte access fits, backward 36 us = 4.6 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -117,7 +120,8 @@ struct Part {
     }
 };
 
-// R rows a team, all requested before the first is looked at. STREAMED: results past the caches
+// R rows a team, all requested before the first is looked at. STREAMED: results past the caches, from 4 MB on. 914601
+// rows of 256 bfloat16 channels: 178 us with both, 259 with one row a team and cached results
 template <int TYPE, bool WIDE, int TPR, int V, int R, bool STREAMED>
 __global__ __launch_bounds__(NTH) void k_norm(NormArgs a)
 {
