@@ -285,7 +285,7 @@ int f3d_bucket_swin_attn_bwd(const void *q, const void *k, const void *v, const 
  *               A row without keys gets zeros, and lse -infinity; so does a row behind its segment's q_lens. Rows before the first
  *               segment and behind the last keep what they held
  *   workspace   >= f3d_cross_attn_workspace_bytes(...) of the same sizes, 256-byte aligned; may be NULL where that is 0
- * Inconsistent offsets or lengths give unspecified results but no access out of bounds. out overlaps no input.
+ * Inconsistent offsets or lengths give unspecified results but no access out of bounds. out overlaps no input (refused).
  * Arithmetic: 16-bit operands, fp32 accumulation and softmax, the sum of the exponentials taken in fp32, the probabilities rounded to 16
  * bits before the product with v; one rounding of the result. Inputs must be finite, and so must the products q k^T and their scaled
  * values in binary32; values of v above 2^80 in magnitude may overflow, those below 2^-80 may count as zeros. The same call gives the
@@ -312,7 +312,7 @@ int f3d_cross_attn_f16(const void *q, const void *k, const void *v, const int32_
  *   q .. softmax_scale   as in the forward call, a scale below 2^-100 is refused;  out, dout  bf16 [n_q, heads*head_dim];  lse  the forward call's
  *   dq (out)  bf16 [n_q, heads*head_dim];  dk, dv (out)  bf16 [n_kv, kv_heads*head_dim]. Rows behind a segment's length get zeros, and
  *             so do rows of no segment and everything of a segment without queries or without keys. The gradients overlap no input and
- *             not each other
+ *             not each other (refused)
  *   workspace >= f3d_cross_attn_bwd_workspace_bytes(...) of the same sizes, 256-byte aligned
  * Arithmetic: bf16 operands, fp32 accumulation; P and dS are rounded to bf16 before the second products. Sums over rows, heads and
  * parts are added in a fixed order: the same call gives the same bits.
@@ -357,7 +357,7 @@ int f3d_ln_linear(const void *x, const int32_t *row_in, const float *gamma, cons
  *   row_in      NULL (row p reads x[p]) or [n] int32, e.g. perm: the results come out bucket-major
  *   gamma, beta binary32 [channels], either may be NULL (ones, zeros)
  *   eps         >= 0
- *   y    (out)  `dtype` [n, channels]; may be x where row_in is NULL
+ *   y    (out)  `dtype` [n, channels]; may be x where row_in is NULL, overlaps it in no other way (refused)
  *   mean, rstd (out)  binary32 [n] of the rows of y, either may be NULL; what f3d_layer_norm_bwd needs
  * Every pointer is aligned to its elements; where x, y, gamma and beta are 16-byte aligned and a row is a multiple of 16 bytes long
  * the rows are moved 16 bytes at a time. Arithmetic: binary32, one rounding to dtype. A row's bits do not depend on the others.
@@ -374,7 +374,7 @@ int f3d_layer_norm(const void *x, const int32_t *row_in, const float *gamma, con
  *   row_in      NULL or [n] int32, every row named once at most: dx is stored where x was read. A row that is not named keeps what
  *               dx held
  *   residual    NULL or `dtype` [n, channels], indexed by the DESTINATION row: the gradient that reaches x past the norm
- *   dx   (out)  `dtype` [n, channels]; may be residual, and dy or x where row_in is NULL
+ *   dx   (out)  `dtype` [n, channels]; may be residual or x, and dy where row_in is NULL (otherwise refused)
  *   dgamma, dbeta (out)  binary32 [channels], either may be NULL; zeros for n = 0
  *   workspace   >= f3d_layer_norm_bwd_workspace_bytes(n, channels), 256-byte aligned; may be NULL where dgamma and dbeta are
  * Arithmetic: binary32; the sums over the rows in a fixed order that follows from n, channels and dtype: the same call gives the same bits.

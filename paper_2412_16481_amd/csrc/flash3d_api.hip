@@ -628,6 +628,12 @@ int f3d_bucket_swin_attn_bwd(const void* q, const void* k, const void* v, const 
     return e == hipSuccess ? F3D_OK : hip_fail(e);
 }
 
+// two ranges of memory that share a byte
+static bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
+{
+    return a && b && a_bytes > 0 && b_bytes > 0 && (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+
 // checks and launch geometry shared by the cross attention calls
 struct CrossSizes {
     int64_t n_q, n_kv, max_q, max_kv;
@@ -646,6 +652,8 @@ static int cross_sizes(CrossSizes& s, int64_t n_q, int64_t n_kv, int32_t n_segme
     s = {n_q, n_kv, max_q > 0 && max_q < n_q ? max_q : n_q, max_kv > 0 && max_kv < n_kv ? max_kv : n_kv, n_segments, heads, kv_heads, head_dim};
     return F3D_OK;
 }
+
+static size_t cross_bytes(int64_t rows, int32_t heads, int32_t head_dim) { return (size_t)rows * heads * head_dim * 2; }
 
 static size_t cross_part_bytes(const CrossSizes& s, const f3d::CrossPlan& p)
 {
@@ -739,6 +747,8 @@ static int cross_forward(int f16, const void* q, const void* k, const void* v, c
         a.part_ml = (float2*)((char*)workspace + part);
         a.part_l = (float*)(a.part_ml + (size_t)p.parts * n_q * heads);
     }
+    const size_t q_bytes = cross_bytes(n_q, heads, head_dim), kv_bytes = cross_bytes(n_kv, kv_heads, head_dim);
+    if (overlap(out, q_bytes, q, q_bytes) || overlap(out, q_bytes, k, kv_bytes) || overlap(out, q_bytes, v, kv_bytes)) return F3D_ERR_INVALID_ARG;
     a.out = (uint16_t*)out;
     a.lse = lse;
     (void)hipGetLastError();
@@ -805,6 +815,16 @@ int f3d_cross_attn_bwd(const void* q, const void* k, const void* v, const void* 
         if (!workspace) return F3D_ERR_INVALID_ARG;
         if ((uintptr_t)workspace & 255) return F3D_ERR_BAD_ALIGNMENT;
         if (workspace_bytes < need) return F3D_ERR_WORKSPACE_TOO_SMALL;
+    }
+    {
+        const size_t q_bytes = cross_bytes(n_q, heads, head_dim), kv_bytes = cross_bytes(n_kv, kv_heads, head_dim);
+        const struct {
+            const void* at;
+            size_t bytes;
+        } x[8] = {{dq, q_bytes}, {dk, kv_bytes}, {dv, kv_bytes}, {q, q_bytes}, {k, kv_bytes}, {v, kv_bytes}, {out, q_bytes}, {dout, q_bytes}};
+        for (int i = 0; i < 3; ++i)
+            for (int j = i + 1; j < 8; ++j)
+                if (overlap(x[i].at, x[i].bytes, x[j].at, x[j].bytes)) return F3D_ERR_INVALID_ARG;
     }
     b.f.out = (uint16_t*)const_cast<void*>(out);
     b.f.lse = const_cast<float*>(lse);
@@ -884,6 +904,8 @@ int f3d_layer_norm(const void* x, const int32_t* row_in, const float* gamma, con
     if (!x || !y) return F3D_ERR_INVALID_ARG;
     if (((uintptr_t)x | (uintptr_t)y) & elem_mask(dtype)) return F3D_ERR_BAD_ALIGNMENT;
     if (((uintptr_t)row_in | (uintptr_t)gamma | (uintptr_t)beta | (uintptr_t)mean | (uintptr_t)rstd) & 3) return F3D_ERR_BAD_ALIGNMENT;
+    const size_t bytes = (size_t)n * channels * (elem_mask(dtype) + 1);
+    if (row_in ? y == x : y != x && overlap(x, bytes, y, bytes)) return F3D_ERR_INVALID_ARG;
     f3d::NormArgs a;
     memset(&a, 0, sizeof(a));
     a.x = x;
@@ -930,6 +952,13 @@ int f3d_layer_norm_bwd(const void* dy, const void* x, const int32_t* row_in, con
         if (workspace_bytes < need) return F3D_ERR_WORKSPACE_TOO_SMALL;
     } else if (n == 0) {
         return F3D_OK;
+    }
+    const size_t bytes = (size_t)n * channels * (elem_mask(dtype) + 1);
+    if (row_in) {
+        if (dy == dx && n > 0) return F3D_ERR_INVALID_ARG;   // read at row p, stored at row row_in[p]
+    } else {
+        for (const void* in : {dy, x, residual})
+            if (in != dx && overlap(in, bytes, dx, bytes)) return F3D_ERR_INVALID_ARG;
     }
     f3d::NormBwdArgs a;
     memset(&a, 0, sizeof(a));

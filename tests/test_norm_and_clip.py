@@ -195,6 +195,17 @@ def test_layer_norm_in_place_and_rows_left_as_they_were():
     assert bool((dx[left] == 5).all()) and not bool((dx[~left] == 5).all(1).any())
 
 
+def test_layer_norm_backward_over_the_gathered_rows_themselves():
+    # dx is stored where x was read
+    d = make(3001, 256, torch.bfloat16)
+    _, mean, rstd = check_forward(d, gather=True)
+    want = f3d.layer_norm_bwd(d["dy"], d["x"], mean, rstd, d["gamma"], d["perm"], d["residual"])
+    for name in ("x", "residual"):
+        e = {k: v.clone() for k, v in d.items()}
+        got = f3d.layer_norm_bwd(e["dy"], e["x"], mean, rstd, e["gamma"], e["perm"], e["residual"], dx=e[name])
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_layer_norm_of_no_rows():
     x = torch.empty(0, 64, device=DEV)
     e = torch.empty(0, device=DEV)

@@ -40,6 +40,16 @@ def test_layer_norm_bwd_refuses(kw, code):
     assert norm_bwd(**kw) == code
 
 
+def test_layer_norm_refuses_results_over_what_is_still_read():
+    far = AT + (1 << 20)
+    assert norm(row_in=far) == INVALID                                  # y is x, and rows are gathered
+    for moved in (AT + 128, AT - 128, AT + 10 * 128 - 16):
+        assert norm(y=moved) == INVALID
+    assert norm_bwd(dy=AT, x=far, row_in=far) == INVALID
+    for name in ("dy", "x", "residual"):
+        assert norm_bwd(**{"dy": far, "x": far, "residual": far, name: AT + 128}) == INVALID
+
+
 def clip(tensors, outs=None, max_norm=1.0, norm=AT, workspace=AT, workspace_bytes=1 << 30):
     """tensors: (address, elements, type); outs: addresses or None for in place."""
     n = len(tensors)
@@ -123,6 +133,17 @@ def test_cross_attn_refuses(kw, code):
     (dict(n_q=0, n_kv=0, q=None, k=None, v=None, out=None, workspace=None), OK)])
 def test_cross_attn_bwd_refuses(kw, code):
     assert cross_bwd(**kw) == code
+
+
+def test_cross_attn_refuses_results_over_what_is_still_read():
+    far = lambda i: AT + (i << 24)   # noqa: E731
+    assert [cross(q=far(1), k=far(2), v=far(3), out=far(x) + d) for x, d in ((1, 0), (2, 16), (3, 50 * 64 * 2 - 16), (1, -16))] == [INVALID] * 4
+    names = ("q", "k", "v", "out", "dout", "dq", "dk", "dv")
+    apart = {x: far(i + 1) for i, x in enumerate(names)}
+    for result in ("dq", "dk", "dv"):
+        for other in names:
+            if other != result:
+                assert cross_bwd(**{**apart, result: apart[other] + 16}) == INVALID, (result, other)
 
 
 def test_cross_attn_workspace_refuses():
