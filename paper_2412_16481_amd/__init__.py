@@ -358,13 +358,12 @@ def _cross_sizes(q, k, v, q_offsets, kv_offsets, heads, head_dim, kv_heads, max_
     _need(q, "q", q.dtype, (n_q, heads * head_dim))
     _need(k, "k", q.dtype, (n_kv, kv_heads * head_dim))
     _need(v, "v", q.dtype, (n_kv, kv_heads * head_dim))
-    segments = {int(t.shape[0]) - less for t, less in ((q_offsets, 1), (kv_offsets, 1), (q_lens, 0), (kv_lens, 0)) if t is not None} or {1}
-    if len(segments) != 1 or ((q_offsets is None or kv_offsets is None) and segments != {1}):
-        raise ValueError("q_offsets, kv_offsets (one more entry than segments), q_lens and kv_lens must be of the same segments")
-    n_segments = segments.pop()
+    # both tensors in one segment, or offsets for both
+    n_segments = 1 if q_offsets is None or kv_offsets is None else int(q_offsets.shape[0]) - 1
     for name, t, n in (("q_offsets", q_offsets, n_segments + 1), ("kv_offsets", kv_offsets, n_segments + 1), ("q_lens", q_lens, n_segments),
                        ("kv_lens", kv_lens, n_segments)):
-        _need(t, name, torch.int32, (n,), optional=True)
+        if t is not None:
+            _need(t, name, torch.int32, (n,))
     return n_q, n_kv, n_segments, max_q, max_kv, heads, kv_heads, head_dim
 
 
