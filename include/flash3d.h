@@ -359,8 +359,8 @@ int f3d_ln_linear(const void *x, const int32_t *row_in, const float *gamma, cons
  *   eps         >= 0
  *   y    (out)  `dtype` [n, channels]; may be x where row_in is NULL, overlaps it in no other way (refused)
  *   mean, rstd (out)  binary32 [n] of the rows of y, either may be NULL; what f3d_layer_norm_bwd needs
- * Every pointer is aligned to its elements; where x, y, gamma and beta are 16-byte aligned and a row is a multiple of 16 bytes long
- * the rows are moved 16 bytes at a time. Arithmetic: binary32, one rounding to dtype. A row's bits do not depend on the others.
+ * Every pointer is aligned to its elements; rows of a multiple of 16 bytes in 16-byte aligned tensors are moved fastest.
+ * Arithmetic: binary32, one rounding to dtype. A row's bits do not depend on the others.
  */
 #define F3D_NORM_MAX_CHANNELS 8192
 int f3d_layer_norm(const void *x, const int32_t *row_in, const float *gamma, const float *beta, float eps, int64_t n,

@@ -16,7 +16,7 @@ struct NormArgs {
     float eps;
     int n, c;
     int type;                 // F3D_BF16 | F3D_F16 | F3D_F32
-    int wide;                 // rows, vectors and weights can be moved 16 bytes at a time
+    int wide;                 // rows and weights begin at multiples of 16 bytes, rows are a multiple long
     void* y;
     float* mean;              // [n], may be null
     float* rstd;

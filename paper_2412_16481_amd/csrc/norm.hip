@@ -13,9 +13,11 @@
 // order: the same call gives the same bits.
 //
 // Bound: HBM. Measured: 914601 rows of 256 bfloat16 channels forward 176 us = 5.3 TB/s, backward with a residual and the weights' gradients
-// 381 us = 4.9 TB/s; 9001 rows of 1537 binary32 channels, which no 16-byte access fits, backward 36 us = 4.6 TB/s.
+// 381 us = 4.9 TB/s; 9001 rows of 1537 binary32 channels, which begin at no multiple of 16 bytes, backward 41 us = 4.0 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "elem.h"
 #include "norm.h"
@@ -57,64 +59,135 @@ __device__ __forceinline__ float2 team_sum2(float v, float w, float* box)
     return make_float2((box[0] + box[1]) + (box[2] + box[3]), (box[4] + box[5]) + (box[6] + box[7]));
 }
 
-// A thread's part of a row: pieces t, t + TPR, .. of W elements. WIDE: 16-byte pieces. Pieces past the row's end count as zeros.
+// A row cut into 16-byte pieces: so many whole ones, and the elements behind them.
+struct Cut {
+    int pieces, rest;
+};
+
+// 16, 8 and 4 bytes at the alignment of 16-bit elements
+typedef u32x4 loose16 __attribute__((aligned(2)));
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef u32x2 loose8 __attribute__((aligned(2)));
+typedef uint32_t loose4 __attribute__((aligned(2)));
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef f32x4 loose_f32x4 __attribute__((aligned(4)));
+
+// A thread's part of a row: pieces t, t + TPR, .. of W elements. What is past the row's end counts as zeros. WIDE: every row begins at a
+// multiple of 16 bytes and is whole pieces. Other rows are moved 16 bytes at a time as well, at whatever address they have; of what
+// is left at the end 16 bytes are read and 8, 4 and 2 written. 100000 rows of 1537 bfloat16 channels forward 170 us, backward 234; element
+// by element 370 and 671 (20000 of 4001 binary32 channels 124 and 189; 150 and 273).
 template <int TYPE, bool WIDE, int TPR, int V>
 struct Part {
     using E = Elems<TYPE>;
     using one = typename E::one;
-    static constexpr int W = WIDE ? E::W : 1;
+    static constexpr int W = E::W;
     static constexpr int N = V * W;                   // elements of a thread
+    static constexpr int PER = 4 / (int)sizeof(one);  // elements of four bytes
+    using piece = typename std::conditional<WIDE, u32x4, loose16>::type;
 
-    static __device__ __forceinline__ void load(const one* row, int t, int pieces, float (&x)[N])
+    static __device__ __forceinline__ Cut cut(int c) { return {c / W, WIDE ? 0 : c % W}; }
+    // elements [0, W) of piece v of this thread that the row has
+    static __device__ __forceinline__ int has(Cut cut, int t, int v)
     {
-        if constexpr (WIDE) {
-            uint4 u[V];
+        const int i = t + v * TPR;
+        return i < cut.pieces ? W : !WIDE && i == cut.pieces ? cut.rest : 0;
+    }
+    static __device__ __forceinline__ uint4 load_rest(const one* at, int rest)
+    {
+        const uint32_t* const p = reinterpret_cast<const uint32_t*>(at);
+        const int words = rest / PER;
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (words & 2) {
+            const u32x2 y = *reinterpret_cast<const loose8*>(p);
+            u.x = y.x;
+            u.y = y.y;
+        }
+        if (words & 1) (words & 2 ? u.z : u.x) = *reinterpret_cast<const loose4*>(p + (words & 2));
+        if (PER == 2 && (rest & 1)) (words == 0 ? u.x : words == 1 ? u.y : words == 2 ? u.z : u.w) = *reinterpret_cast<const uint16_t*>(p + words);
+        return u;
+    }
+    static __device__ __forceinline__ void store_rest(one* at, int rest, const uint4& u)
+    {
+        uint32_t* const p = reinterpret_cast<uint32_t*>(at);
+        const int words = rest / PER;
+        if (words & 2) {
+            const u32x2 y = {u.x, u.y};
+            *reinterpret_cast<loose8*>(p) = y;
+        }
+        if (words & 1) *reinterpret_cast<loose4*>(p + (words & 2)) = words & 2 ? u.z : u.x;
+        if (PER == 2 && (rest & 1)) *reinterpret_cast<uint16_t*>(p + words) = (uint16_t)(words == 0 ? u.x : words == 1 ? u.y : words == 2 ? u.z : u.w);
+    }
+    // the piece without its first `drop` elements, zeros behind
+    static __device__ __forceinline__ uint4 dropped(uint4 u, int drop)
+    {
+        const int words = drop / PER;
+        if (words & 2) u = make_uint4(u.z, u.w, 0, 0);
+        if (words & 1) u = make_uint4(u.y, u.z, u.w, 0);
+        if (PER == 2 && (drop & 1)) u = make_uint4(u.x >> 16 | u.y << 16, u.y >> 16 | u.z << 16, u.z >> 16 | u.w << 16, u.w >> 16);
+        return u;
+    }
+    // The last piece of a row that is no whole pieces is read as the row's last 16 bytes, so that every thread has one load a piece
+    static __device__ __forceinline__ void load(const one* row, int t, Cut cut, float (&x)[N])
+    {
+        const bool shorter = !WIDE && cut.pieces == 0;   // than one piece
+        uint4 u[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) u[v] = t + v * TPR < pieces ? reinterpret_cast<const uint4*>(row)[t + v * TPR] : make_uint4(0, 0, 0, 0);
+        for (int v = 0; v < V; ++v) {
+            const int i = t + v * TPR;
+            u[v] = make_uint4(0, 0, 0, 0);
+            if (i < cut.pieces + (cut.rest != 0) && !shorter) {
+                const int at = WIDE || i < cut.pieces ? i * W : i * W - (W - cut.rest);
+                const u32x4 y = *reinterpret_cast<const piece*>(row + at);
+                u[v] = make_uint4(y.x, y.y, y.z, y.w);
+            }
+        }
+        if (shorter && t == 0 && cut.rest != 0) u[0] = load_rest(row, cut.rest);
 #pragma unroll
-            for (int v = 0; v < V; ++v) E::unpack(u[v], *reinterpret_cast<float(*)[W]>(x + v * W));
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = t + v * TPR < pieces ? E::to_f32(row[t + v * TPR]) : 0.f;
+        for (int v = 0; v < V; ++v) {
+            if (!WIDE && cut.rest != 0 && !shorter && t + v * TPR == cut.pieces) u[v] = dropped(u[v], W - cut.rest);
+            E::unpack(u[v], *reinterpret_cast<float(*)[W]>(x + v * W));
         }
     }
     template <bool STREAMED = false>
-    static __device__ __forceinline__ void store(one* row, int t, int pieces, const float (&x)[N])
+    static __device__ __forceinline__ void store(one* row, int t, Cut cut, const float (&x)[N])
     {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            if (t + v * TPR >= pieces) continue;
-            if constexpr (WIDE) {
-                const uint4 u = E::pack(*reinterpret_cast<const float(*)[W]>(x + v * W));
+            const uint4 u = E::pack(*reinterpret_cast<const float(*)[W]>(x + v * W));
+            if (t + v * TPR < cut.pieces) {
                 const u32x4 y = {u.x, u.y, u.z, u.w};
-                u32x4* const to = reinterpret_cast<u32x4*>(row) + t + v * TPR;
+                piece* const to = reinterpret_cast<piece*>(row) + t + v * TPR;
                 if (STREAMED) __builtin_nontemporal_store(y, to);
                 else *to = y;
-            } else {
-                row[t + v * TPR] = E::from_f32(x[v]);
+            } else if (!WIDE && t + v * TPR == cut.pieces) {
+                store_rest(row + cut.pieces * W, cut.rest, u);
             }
         }
     }
     // the row's weights, `none` where there are none
-    static __device__ __forceinline__ void weights(const float* w, float none, int t, int pieces, float (&x)[N])
+    static __device__ __forceinline__ void weights(const float* w, float none, int t, Cut cut, float (&x)[N])
     {
+        using four = typename std::conditional<WIDE, f32x4, loose_f32x4>::type;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int at = (t + v * TPR) * W;
+            const float* const at = w + (t + v * TPR) * W;
+            const int n = has(cut, t, v);
 #pragma unroll
             for (int e = 0; e < W; ++e) x[v * W + e] = none;
-            if (!w || t + v * TPR >= pieces) continue;
-            if constexpr (WIDE) {
+            if (!w) continue;
+            if (n == W) {
 #pragma unroll
                 for (int e = 0; e < W; e += 4) {
-                    const float4 f = *reinterpret_cast<const float4*>(w + at + e);
+                    const f32x4 f = *reinterpret_cast<const four*>(at + e);
                     x[v * W + e] = f.x;
                     x[v * W + e + 1] = f.y;
                     x[v * W + e + 2] = f.z;
                     x[v * W + e + 3] = f.w;
                 }
-            } else {
-                x[v] = w[at];
+            } else if (!WIDE) {
+#pragma unroll
+                for (int e = 0; e < W - 1; ++e)
+                    if (e < n) x[v * W + e] = at[e];
             }
         }
     }
@@ -131,7 +204,7 @@ __global__ __launch_bounds__(NTH) void k_norm(NormArgs a)
     __shared__ float box[2 * R][8];
     const int t = threadIdx.x % TPR;
     const long long first = (long long)blockIdx.x * (TEAMS * R) + threadIdx.x / TPR;
-    const int pieces = a.c / P::W;
+    const Cut cut = P::cut(a.c);
     size_t r[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
@@ -140,10 +213,10 @@ __global__ __launch_bounds__(NTH) void k_norm(NormArgs a)
     }
     float x[R][P::N];
 #pragma unroll
-    for (int k = 0; k < R; ++k) P::load(static_cast<const one*>(a.x) + r[k] * a.c, t, pieces, x[k]);
+    for (int k = 0; k < R; ++k) P::load(static_cast<const one*>(a.x) + r[k] * a.c, t, cut, x[k]);
     float g[P::N], b[P::N];
-    P::weights(a.gamma, 1.f, t, pieces, g);
-    P::weights(a.beta, 0.f, t, pieces, b);
+    P::weights(a.gamma, 1.f, t, cut, g);
+    P::weights(a.beta, 0.f, t, cut, b);
     const float inv = 1.0f / a.c;
     float mu[R], rs[R];
 #pragma unroll
@@ -158,9 +231,13 @@ __global__ __launch_bounds__(NTH) void k_norm(NormArgs a)
         float q = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            if (t + v * TPR >= pieces) continue;      // the zeros past the end are no elements
+            const int n = P::has(cut, t, v);          // the zeros past the end are no elements
+            if (n == 0) continue;
 #pragma unroll
-            for (int e = 0; e < P::W; ++e) q += (x[k][v * P::W + e] - mu[k]) * (x[k][v * P::W + e] - mu[k]);
+            for (int e = 0; e < P::W; ++e) {
+                const float off = WIDE || e < n ? x[k][v * P::W + e] - mu[k] : 0.f;
+                q += off * off;
+            }
         }
         rs[k] = 1.0f / sqrtf(team_sum<TPR>(q, box[R + k]) * inv + a.eps);
     }
@@ -170,7 +247,7 @@ __global__ __launch_bounds__(NTH) void k_norm(NormArgs a)
         if (p >= a.n) break;
 #pragma unroll
         for (int i = 0; i < P::N; ++i) x[k][i] = (x[k][i] - mu[k]) * rs[k] * g[i] + b[i];
-        P::template store<STREAMED>(static_cast<one*>(a.y) + (size_t)p * a.c, t, pieces, x[k]);
+        P::template store<STREAMED>(static_cast<one*>(a.y) + (size_t)p * a.c, t, cut, x[k]);
         if (t == 0) {
             if (a.mean) a.mean[p] = mu[k];
             if (a.rstd) a.rstd[p] = rs[k];
@@ -187,10 +264,10 @@ __global__ __launch_bounds__(NTH) void k_norm_bwd(NormBwdArgs a)
     constexpr int TEAMS = NTH / TPR;
     __shared__ float box[2 * R][8];
     const int t = threadIdx.x % TPR;
-    const int pieces = a.c / P::W;
+    const Cut cut = P::cut(a.c);
     const float inv = 1.0f / a.c;
     float g[P::N], dg[P::N], db[P::N];
-    P::weights(a.gamma, 1.f, t, pieces, g);
+    P::weights(a.gamma, 1.f, t, cut, g);
 #pragma unroll
     for (int i = 0; i < P::N; ++i) dg[i] = db[i] = 0.f;
     int turn = 0;
@@ -204,10 +281,10 @@ __global__ __launch_bounds__(NTH) void k_norm_bwd(NormBwdArgs a)
             r[k] = (size_t)(has && a.row_in ? a.row_in[p] : p);
             mu[k] = has ? a.mean[p] : 0.f;
             rs[k] = has ? a.rstd[p] : 0.f;
-            P::load(static_cast<const one*>(a.dy) + (size_t)p * a.c, t, has ? pieces : 0, dy[k]);
+            P::load(static_cast<const one*>(a.dy) + (size_t)p * a.c, t, has ? cut : Cut{0, 0}, dy[k]);
         }
 #pragma unroll
-        for (int k = 0; k < R; ++k) P::load(static_cast<const one*>(a.x) + r[k] * a.c, t, first + k * TEAMS < a.n ? pieces : 0, x[k]);
+        for (int k = 0; k < R; ++k) P::load(static_cast<const one*>(a.x) + r[k] * a.c, t, first + k * TEAMS < a.n ? cut : Cut{0, 0}, x[k]);
         float m1[R], m2[R];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
@@ -233,11 +310,11 @@ __global__ __launch_bounds__(NTH) void k_norm_bwd(NormBwdArgs a)
 #pragma unroll
             for (int i = 0; i < P::N; ++i) dy[k][i] = rs[k] * (dy[k][i] - m1[k] - x[k][i] * m2[k]);
             if (a.residual) {
-                P::load(static_cast<const one*>(a.residual) + r[k] * a.c, t, pieces, x[k]);
+                P::load(static_cast<const one*>(a.residual) + r[k] * a.c, t, cut, x[k]);
 #pragma unroll
                 for (int i = 0; i < P::N; ++i) dy[k][i] += x[k][i];
             }
-            P::template store<STREAMED>(static_cast<one*>(a.dx) + r[k] * a.c, t, pieces, dy[k]);
+            P::template store<STREAMED>(static_cast<one*>(a.dx) + r[k] * a.c, t, cut, dy[k]);
         }
     }
     if (!WEIGHTS) return;
@@ -261,10 +338,10 @@ __global__ __launch_bounds__(NTH) void k_norm_bwd(NormBwdArgs a)
                 u += meet[0][k * TPR + t];
                 w += meet[1][k * TPR + t];
             }
-            const int piece = t + i / P::W * TPR;
-            if (piece < pieces) {
-                if (gamma_to) gamma_to[piece * P::W + i % P::W] = u;
-                if (beta_to) beta_to[piece * P::W + i % P::W] = w;
+            const int col = (t + i / P::W * TPR) * P::W + i % P::W;
+            if (col < a.c) {
+                if (gamma_to) gamma_to[col] = u;
+                if (beta_to) beta_to[col] = w;
             }
         }
     }
@@ -303,10 +380,12 @@ struct Forward {
     template <int TYPE, bool WIDE, int TPR, int V>
     hipError_t go() const
     {
-        constexpr int TEAMS = NTH / TPR, R = TPR == 256 || !WIDE ? 1 : 4 / V;
+        constexpr int TEAMS = NTH / TPR;
+        // four rows on their way a wave; two of a workgroup's where a thread has up to 16 of their 16-bit elements (40000 rows of 4096 127 -> 113 us)
+        constexpr int R = TPR == 256 ? (TYPE != F3D_F32 && V <= 2 ? 2 : 1) : 4 / V;
         const long long steps = ((long long)a.n + TEAMS - 1) / TEAMS;
-        if (WIDE && (size_t)a.n * a.c * sizeof(typename Elems<TYPE>::one) >= STREAMED_BYTES)
-            k_norm<TYPE, WIDE, TPR, V, R, WIDE><<<(unsigned)((steps + R - 1) / R), NTH, 0, stream>>>(a);
+        if ((size_t)a.n * a.c * sizeof(typename Elems<TYPE>::one) >= STREAMED_BYTES)
+            k_norm<TYPE, WIDE, TPR, V, R, true><<<(unsigned)((steps + R - 1) / R), NTH, 0, stream>>>(a);
         else
             k_norm<TYPE, WIDE, TPR, V, 1, false><<<(unsigned)steps, NTH, 0, stream>>>(a);
         return hipGetLastError();
@@ -337,47 +416,41 @@ struct Backward {
     template <int TYPE, bool WIDE, int TPR, int V>
     hipError_t go() const
     {
-        constexpr int R = TPR == 256 || !WIDE || V > 2 ? 1 : 2;
+        constexpr int R = (TPR == 256 && V > 1) || V > 2 ? 1 : 2;
         const bool large = (size_t)a.n * a.c * sizeof(typename Elems<TYPE>::one) >= STREAMED_BYTES;
-        if constexpr (WIDE) {
-            if (large) return with<TYPE, WIDE, TPR, V, R, true>();
-        }
-        return with<TYPE, WIDE, TPR, V, 1, false>();
+        return large ? with<TYPE, WIDE, TPR, V, R, true>() : with<TYPE, WIDE, TPR, V, 1, false>();
     }
 };
 
 // A team is as small as keeps a thread's part of a row in one 16-byte piece, up to a wave, then the parts grow to four pieces, then
-// a workgroup takes the row. Rows that cannot be moved 16 bytes at a time go element by element.
-template <int TYPE, class F>
-hipError_t by_width(const F& f, int c, int wide)
+// a workgroup takes the row. Parts of 32 elements leave no registers for rows of any alignment: 100000 rows of 1537 bfloat16 channels,
+// backward, 314 us by a wave, 234 by a workgroup.
+template <int TYPE, bool WIDE, class F>
+hipError_t by_width(const F& f, int c)
 {
-    if (wide) {
-        const int pieces = c / Elems<TYPE>::W;
-        if (pieces <= 8) return f.template go<TYPE, true, 8, 1>();
-        if (pieces <= 16) return f.template go<TYPE, true, 16, 1>();
-        if (pieces <= 32) return f.template go<TYPE, true, 32, 1>();
-        if (pieces <= 64) return f.template go<TYPE, true, 64, 1>();
-        if (pieces <= 128) return f.template go<TYPE, true, 64, 2>();
-        if (pieces <= 256) return f.template go<TYPE, true, 64, 4>();
-        if (pieces <= 512) return f.template go<TYPE, true, 256, 2>();
-        if (pieces <= 1024) return f.template go<TYPE, true, 256, 4>();
-        if constexpr (TYPE == F3D_F32) return f.template go<TYPE, true, 256, 8>();
-        return hipErrorInvalidValue;
+    const int pieces = (c + Elems<TYPE>::W - 1) / Elems<TYPE>::W;
+    if (pieces <= 8) return f.template go<TYPE, WIDE, 8, 1>();
+    if (pieces <= 16) return f.template go<TYPE, WIDE, 16, 1>();
+    if (pieces <= 32) return f.template go<TYPE, WIDE, 32, 1>();
+    if (pieces <= 64) return f.template go<TYPE, WIDE, 64, 1>();
+    if (pieces <= 128) return f.template go<TYPE, WIDE, 64, 2>();
+    if (pieces <= 256) {
+        if constexpr (WIDE || TYPE == F3D_F32) return f.template go<TYPE, WIDE, 64, 4>();
+        else return f.template go<TYPE, WIDE, 256, 1>();
     }
-    if (c <= 64) return f.template go<TYPE, false, 64, 1>();
-    if (c <= 256) return f.template go<TYPE, false, 64, 4>();
-    if (c <= 1024) return f.template go<TYPE, false, 64, 16>();
-    if (c <= 2048) return f.template go<TYPE, false, 256, 8>();
-    return f.template go<TYPE, false, 256, 32>();
+    if (pieces <= 512) return f.template go<TYPE, WIDE, 256, 2>();
+    if (pieces <= 1024) return f.template go<TYPE, WIDE, 256, 4>();
+    if constexpr (TYPE == F3D_F32) return f.template go<TYPE, WIDE, 256, 8>();
+    return hipErrorInvalidValue;
 }
 
 template <class F>
 hipError_t by_type(const F& f, int type, int c, int wide)
 {
     switch (type) {
-        case F3D_BF16: return by_width<F3D_BF16>(f, c, wide);
-        case F3D_F16: return by_width<F3D_F16>(f, c, wide);
-        default: return by_width<F3D_F32>(f, c, wide);
+        case F3D_BF16: return wide ? by_width<F3D_BF16, true>(f, c) : by_width<F3D_BF16, false>(f, c);
+        case F3D_F16: return wide ? by_width<F3D_F16, true>(f, c) : by_width<F3D_F16, false>(f, c);
+        default: return wide ? by_width<F3D_F32, true>(f, c) : by_width<F3D_F32, false>(f, c);
     }
 }
 

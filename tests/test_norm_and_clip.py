@@ -195,6 +195,23 @@ def test_layer_norm_in_place_and_rows_left_as_they_were():
     assert bool((dx[left] == 5).all()) and not bool((dx[~left] == 5).all(1).any())
 
 
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("c", [3, 13, 101, 1537, 4095])
+def test_layer_norm_in_place_with_rows_of_any_alignment(c, t):
+    # the end of a row is read 16 bytes at a time, beside what others of the row have stored already
+    for n in (5, 3000):
+        d = make(n, c, TYPES[t])
+        want, mean, rstd = check_forward(d)
+        x = d["x"].clone()
+        assert torch.equal(f3d.layer_norm(x, d["gamma"], d["beta"], out=x), want)
+        check_backward(d, mean, rstd, residual=True)
+        want = f3d.layer_norm_bwd(d["dy"], d["x"], mean, rstd, d["gamma"], residual=d["residual"])
+        for name in ("residual", "dy", "x"):
+            e = {k: v.clone() for k, v in d.items()}
+            got = f3d.layer_norm_bwd(e["dy"], e["x"], mean, rstd, e["gamma"], residual=e["residual"], dx=e[name])
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), name
+
+
 def test_layer_norm_backward_over_the_gathered_rows_themselves():
     # dx is stored where x was read
     d = make(3001, 256, torch.bfloat16)
