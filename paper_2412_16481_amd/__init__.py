@@ -377,12 +377,14 @@ def cross_attn(q, k, v, q_offsets, kv_offsets, heads: int, head_dim: int, kv_hea
     sizes = _cross_sizes(q, k, v, q_offsets, kv_offsets, heads, head_dim, kv_heads, max_q, max_kv, q_lens, kv_lens)
     if out is None:
         out = torch.empty_like(q)
-    _need(out, "out", q.dtype, tuple(q.shape))
+    else:
+        _need(out, "out", q.dtype, tuple(q.shape))
     _need(lse, "lse", torch.float32, (sizes[0], heads), optional=True)
     if workspace is None:
         need = cross_attn_workspace_bytes(*sizes)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    _need(workspace, "workspace", torch.uint8, (None,), optional=True)
+    else:
+        _need(workspace, "workspace", torch.uint8, (None,))
     _here(q, k, v, q_offsets, kv_offsets, q_lens, kv_lens, out, lse, workspace)
     entry = lib().f3d_cross_attn if q.dtype == torch.bfloat16 else lib().f3d_cross_attn_f16
     rc = entry(_ptr(q), _ptr(k), _ptr(v), _ptr(q_offsets), _ptr(kv_offsets), _ptr(q_lens), _ptr(kv_lens), *sizes, softmax_scale, _ptr(out),
@@ -398,12 +400,13 @@ def cross_attn_bwd(q, k, v, out, dout, lse, q_offsets, kv_offsets, heads: int, h
     import torch
     sizes = _cross_sizes(q, k, v, q_offsets, kv_offsets, heads, head_dim, kv_heads, max_q, max_kv, q_lens, kv_lens)
     for name, t in (("q", q), ("out", out), ("dout", dout)):
-        _need(t, name, torch.bfloat16, tuple(q.shape))
+        _need(t, name, torch.bfloat16, (sizes[0], heads * head_dim))
     _need(lse, "lse", torch.float32, (sizes[0], heads))
     dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     if workspace is None:
         workspace = torch.empty(max(cross_attn_workspace_bytes(*sizes, backward=True), 256), dtype=torch.uint8, device=q.device)
-    _need(workspace, "workspace", torch.uint8, (None,))
+    else:
+        _need(workspace, "workspace", torch.uint8, (None,))
     _here(q, k, v, out, dout, lse, q_offsets, kv_offsets, q_lens, kv_lens, workspace)
     rc = lib().f3d_cross_attn_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(dout), _ptr(lse), _ptr(q_offsets), _ptr(kv_offsets), _ptr(q_lens),
                                   _ptr(kv_lens), *sizes, softmax_scale, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace), workspace.numel(),
@@ -466,7 +469,8 @@ def layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, row_in=None, out=Non
     _need(row_in, "row_in", torch.int32, (n,), optional=True)
     if out is None:
         out = torch.empty_like(x)
-    _need(out, "out", x.dtype, (n, c))
+    else:
+        _need(out, "out", x.dtype, (n, c))
     _need(mean, "mean", torch.float32, (n,), optional=True)
     _need(rstd, "rstd", torch.float32, (n,), optional=True)
     _here(x, gamma, beta, row_in, out, mean, rstd)
@@ -501,12 +505,14 @@ def layer_norm_bwd(dy, x, mean, rstd, gamma=None, row_in=None, residual=None, we
     _need(residual, "residual", x.dtype, (n, c), optional=True)
     if dx is None:
         dx = torch.empty_like(x)
-    _need(dx, "dx", x.dtype, (n, c))
+    else:
+        _need(dx, "dx", x.dtype, (n, c))
     dgamma = torch.empty(c, dtype=torch.float32, device=x.device) if weight_grads else None
-    dbeta = torch.empty(c, dtype=torch.float32, device=x.device) if weight_grads else None
-    if workspace is None and weight_grads:
+    dbeta = torch.empty_like(dgamma) if weight_grads else None
+    if workspace is not None:
+        _need(workspace, "workspace", torch.uint8, (None,))
+    elif weight_grads:
         workspace = torch.empty(layer_norm_bwd_workspace_bytes(n, c), dtype=torch.uint8, device=x.device)
-    _need(workspace, "workspace", torch.uint8, (None,), optional=True)
     _here(dy, x, mean, rstd, gamma, row_in, residual, dx, workspace)
     rc = lib().f3d_layer_norm_bwd(_ptr(dy), _ptr(x), _ptr(row_in), _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(residual), n, c,
                                   _dtypes()[x.dtype], _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(workspace),
@@ -551,10 +557,12 @@ def clip_grads(grads, max_norm: float, outs=None, norm=None, workspace=None):
     to = None if outs is None else array("Q", map(T.data_ptr, outs))
     if norm is None:
         norm = torch.empty(1, dtype=torch.float32, device=device)
-    _need(norm, "norm", torch.float32, (1,))
+    else:
+        _need(norm, "norm", torch.float32, (1,))
     if workspace is None:
         workspace = torch.empty(clip_grads_workspace_bytes(n), dtype=torch.uint8, device=device)
-    _need(workspace, "workspace", torch.uint8, (None,))
+    else:
+        _need(workspace, "workspace", torch.uint8, (None,))
     _here(norm, workspace)
     rc = lib().f3d_clip_grads(_at(ins), _at(to), _at(sizes), _at(codes), n, max_norm, _ptr(norm), _ptr(workspace), workspace.numel(), _stream())
     if rc != F3D_OK:
