@@ -476,37 +476,73 @@ __global__ __launch_bounds__(64 * FewStage<D>::WAVES, D == 128 ? 1 : 2) void k_c
     }
 }
 
-// The parts of every (row, head): D / 4 threads, four channels each. 4.8 us at the sizes above.
-template <int D, bool F16>
+// The parts of every (row, head): D / 4 threads with four channels each, GROUPS times over where there are many parts: every group takes each
+// GROUPS-th part and they meet in LDS. With the kernel in front, one query over 60000 states of 8 x 128 channels 55 us, 110 with one group;
+// four queries over 3000 of 8 x 64 12 and 18.
+template <int D, bool F16, int GROUPS>
 __global__ __launch_bounds__(256) void k_cross_join(CrossArgs a)
 {
-    constexpr int TPR = D / 4;
-    const long long n = (long long)a.n_q * a.H, at = (long long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-    const int c = (threadIdx.x % TPR) * 4;
-    if (at >= n) return;
+    constexpr int TPR = D / 4, ROWS = 256 / (TPR * GROUPS);
+    struct Sums {
+        float top, sum, whole, y[4];                  // the parts' largest score, sums relative to it
+    };
+    __shared__ Sums meet[GROUPS > 1 ? GROUPS - 1 : 1][ROWS * TPR];
+    const int x = threadIdx.x % (ROWS * TPR), k = threadIdx.x / (ROWS * TPR);
+    const long long n = (long long)a.n_q * a.H, at = (long long)blockIdx.x * ROWS + x / TPR;
+    const int c = (x % TPR) * 4;
     // rows behind the last segment, or before the first, belong to nobody: they stay as they were
-    const long long q = at / a.H;
-    if (q < offset_of(a.q_offsets, a.n_q, 0) || q >= offset_of(a.q_offsets, a.n_q, a.segments)) return;
-    float top = -INFINITY;
-    for (int p = 0; p < a.parts; ++p) top = fmaxf(top, a.part_ml[p * n + at].x);
-    float sum = 0.f, whole = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+    const long long q = min(at, n - 1) / a.H;
+    const bool has = at < n && q >= offset_of(a.q_offsets, a.n_q, 0) && q < offset_of(a.q_offsets, a.n_q, a.segments);
+    Sums s = {-INFINITY, 0.f, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    if (has) {
 #pragma unroll 4
-    for (int p = 0; p < a.parts; ++p) {
-        const float2 ml = a.part_ml[p * n + at];
-        if (ml.x == -INFINITY) continue;              // no keys in this part: nothing was stored
-        const float w = __builtin_amdgcn_exp2f(ml.x - top);
-        const float4 o = *reinterpret_cast<const float4*>(a.part_o + (p * n + at) * D + c);
-        sum += w * ml.y;
-        if (a.lse) whole += w * a.part_l[p * n + at];
-        y[0] += w * o.x;
-        y[1] += w * o.y;
-        y[2] += w * o.z;
-        y[3] += w * o.w;
+        for (int p = k; p < a.parts; p += GROUPS) s.top = fmaxf(s.top, a.part_ml[p * n + at].x);
+#pragma unroll 4
+        for (int p = k; p < a.parts; p += GROUPS) {
+            const float2 ml = a.part_ml[p * n + at];
+            if (ml.x == -INFINITY) continue;          // no keys in this part: nothing was stored
+            const float w = __builtin_amdgcn_exp2f(ml.x - s.top);
+            const float4 o = *reinterpret_cast<const float4*>(a.part_o + (p * n + at) * D + c);
+            s.sum += w * ml.y;
+            if (a.lse) s.whole += w * a.part_l[p * n + at];
+            s.y[0] += w * o.x;
+            s.y[1] += w * o.y;
+            s.y[2] += w * o.z;
+            s.y[3] += w * o.w;
+        }
     }
-    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-    if (a.lse && c == 0) a.lse[at] = sum > 0.f ? (top + __log2f(whole)) * LN2 : -INFINITY;
+    if (GROUPS > 1) {
+        if (k > 0) meet[k - 1][x] = s;
+        __syncthreads();
+        if (k > 0) return;
+        float top = s.top;
+#pragma unroll
+        for (int g = 0; g < GROUPS - 1; ++g) top = fmaxf(top, meet[g][x].top);
+        Sums all = {top, 0.f, 0.f, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            const Sums t = g == 0 ? s : meet[g > 0 ? g - 1 : 0][x];
+            const float w = t.top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(t.top - top);
+            all.sum += w * t.sum;
+            all.whole += w * t.whole;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) all.y[e] += w * t.y[e];
+        }
+        s = all;
+    }
+    if (!has) return;
+    const float inv = s.sum > 0.f ? 1.0f / s.sum : 0.f;
+    if (a.lse && c == 0) a.lse[at] = s.sum > 0.f ? (s.top + __log2f(s.whole)) * LN2 : -INFINITY;
     *reinterpret_cast<uint2*>(a.out + at * D + c) =
-        make_uint2(Half<F16>::pack(y[0] * inv, y[1] * inv), Half<F16>::pack(y[2] * inv, y[3] * inv));
+        make_uint2(Half<F16>::pack(s.y[0] * inv, s.y[1] * inv), Half<F16>::pack(s.y[2] * inv, s.y[3] * inv));
+}
+
+template <int D, bool F16, int GROUPS>
+hipError_t join(const CrossArgs& a, hipStream_t stream)
+{
+    constexpr int ROWS = 256 / (D / 4 * GROUPS);
+    k_cross_join<D, F16, GROUPS><<<(unsigned)(((long long)a.n_q * a.H + ROWS - 1) / ROWS), 256, 0, stream>>>(a);
+    return hipGetLastError();
 }
 
 template <int D, bool F16>
@@ -526,9 +562,7 @@ hipError_t launch(const CrossArgs& a, hipStream_t stream)
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !split) return e;
-    constexpr int PER = 256 / (D / 4);
-    k_cross_join<D, F16><<<(unsigned)(((long long)a.n_q * a.H + PER - 1) / PER), 256, 0, stream>>>(a);
-    return hipGetLastError();
+    return a.parts < 4 ? join<D, F16, 1>(a, stream) : join<D, F16, 8>(a, stream);
 }
 
 template <int D>
@@ -547,13 +581,15 @@ CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_
     const long long rows = n_q * group;               // of one key/value head
     p.few = max_q * group <= 32 && !backward;
     const int block_shift = p.few ? 5 : 7;            // the tile of one wave, or of four
-    // fewer than two workgroups per compute unit: parts of 256 keys at least, until there are about three
+    // Parts of 256 keys at least. Single rows: where there are fewer than two workgroups per compute unit, until there are about three (the
+    // loads of a cache in flight). Rows' blocks: only until every compute unit has one: 4096 x 300 keys of 8 x 32 channels (256 blocks)
+    // 8.0 us, 14.4 with three; 512 x 8000 of 8 x 128 (32 blocks) 37 and 56; 2000 x 4000 of 8 x 64 (128 blocks) 38 and 40.
     long long work = (rows + (1ll << block_shift) - 1) >> block_shift;
     if (work < segments) work = segments;
     const long long blocks = work * kv_heads;
     long long parts = 1;
-    if (blocks < 2 * CUS) {
-        parts = (3 * CUS + blocks - 1) / blocks;
+    if (blocks < (p.few ? 2 * CUS : CUS)) {
+        parts = ((p.few ? 3 * CUS : CUS) + blocks - 1) / blocks;
         const long long most = (max_kv + 255) / 256;
         if (parts > most) parts = most;
         if (parts < 1) parts = 1;
@@ -583,8 +619,10 @@ CrossPlan cross_plan(long long n_q, long long n_kv, int segments, long long max_
     p.kv_slots = (int)(n_kv / 128 + segments);
     const long long kv_work = n_kv / 128 > segments ? n_kv / 128 : segments;
     long long row_parts = 1;
+    // fewer than two workgroups per compute unit: until there are one and a half (two segments of 700 rows and 2000 keys, 32 heads of 128
+    // channels on 8: 216 us for all gradients, 246 with three; 50000 rows and 500 keys, 8 of 128: 461 and 501)
     if (kv_work * kv_heads < 2 * CUS) {
-        row_parts = (3 * CUS + kv_work * kv_heads - 1) / (kv_work * kv_heads);
+        row_parts = (3 * CUS / 2 + kv_work * kv_heads - 1) / (kv_work * kv_heads);
         const long long most = (max_q * group + 255) / 256;
         if (row_parts > most) row_parts = most;
         if (row_parts < 1) row_parts = 1;
