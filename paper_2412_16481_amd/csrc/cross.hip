@@ -75,15 +75,15 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a)
     const float mul = a.s_mul;
 
     // this lane's row: row l32 of the wave's tile
-    U4 qf[KS];
+    U4 qf[KS], nq[KS];
     auto row_of = [&](int blk) __attribute__((always_inline)) { return first_row + blk * BM + wave * 32 + l32; };
-    uint32_t place;                                   // (query, head) of the tensor
+    uint32_t place, next_place;                       // (query, head) of the tensor
     auto fetch_row = [&](int blk) __attribute__((always_inline)) {
         const int r = min(row_of(blk), rows - 1), i = divide(r, a.G, a.by_g), g = r - i * a.G;   // past the end: the last row
-        place = (uint32_t)(qs.from + i) * (uint32_t)a.H + (uint32_t)(kh * a.G + g);
-        const char* const from = reinterpret_cast<const char*>(a.q) + (uint64_t)place * T::ROWB + hf * 16;
+        next_place = (uint32_t)(qs.from + i) * (uint32_t)a.H + (uint32_t)(kh * a.G + g);
+        const char* const from = reinterpret_cast<const char*>(a.q) + (uint64_t)next_place * T::ROWB + hf * 16;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) qf[ks].u = *reinterpret_cast<const uint4*>(from + ks * 32);
+        for (int ks = 0; ks < KS; ++ks) nq[ks].u = *reinterpret_cast<const uint4*>(from + ks * 32);
     };
     fetch_row(0);
     if (nkeys > 0) {
@@ -207,6 +207,10 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a)
     };
     for (int blk = 0; blk < blocks; ++blk) {
         const bool busy = first_row + blk * BM + wave * 32 < live;   // this wave has rows with results
+        place = next_place;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[ks] = nq[ks];
+        if (blk + 1 < blocks) fetch_row(blk + 1);
         robust = false;
         while (nkeys > 0) {
             sweep(busy);
@@ -224,11 +228,10 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a)
                 __syncthreads();
             }
         }
-        // ---- results; the next block's rows are on their way meanwhile
+        // ---- results
         const int row = row_of(blk);
         const bool has = row < live && nkeys > 0;
         const uint32_t at_q = place;
-        if (blk + 1 < blocks) fetch_row(blk + 1);
         if (row >= rows) continue;
         if (SPLIT) {
             const size_t pa = (size_t)part * a.n_q * a.H + at_q;
