@@ -33,9 +33,9 @@ constexpr float LN2 = 0.6931471805599453f;
 // the fixed reference 0, without a maximum to find and to move; a block whose sums leave the safe range is done again with the running
 // maximum (reference moved only by more than 2^8). Bound: the vector ALU's issue port. A tile of 32 channels has 16 exponentials (8
 // cycles each), 34 other instructions and 4 MFMAs (16 cycles of the same port each), 16 more with lse. Measured: 914601 rows of 8 x 32
-// channels, 256 keys a segment, lse: 470 us = 511 TFLOP/s; about 7000 keys: 635 TFLOP/s; 16 ragged segments of up to 2047 rows and 1500 keys,
+// channels, 256 keys a segment, lse: 467 us = 513 TFLOP/s; about 7000 keys: 635 TFLOP/s; 16 ragged segments of up to 2047 rows and 1500 keys,
 // 12 heads of 64 channels on 4, binary16: 102 us = 730 TFLOP/s (121 with the running maximum in the first sweep, and 516 for the
-// other); two segments of 60000 rows and 300 keys, 8 x 128 channels: 281 us = 525 TFLOP/s (322 with one workgroup on a compute unit).
+// other); two segments of 60000 rows and 300 keys, 8 x 128 channels: 275 us = 536 TFLOP/s (322 with one workgroup on a compute unit).
 template <int D, bool F16, bool SPLIT, bool LSE>
 __global__ __launch_bounds__(256, 2) void k_cross(CrossArgs a)
 {
